@@ -387,6 +387,124 @@ qp_status qp_controller_init(qp_controller_t *c, uint32_t window, double s_image
  * QP_EINVAL on null pointers or non-positive / NaN payload_bits or seconds (the record is unchanged). */
 qp_status qp_controller_update(qp_controller_t *c, double payload_bits, double seconds, uint32_t *q_next);
 
+/* ==== a key/value cache held in 4 bits ==================================================
+ * What attention keeps of the tokens that a pipeline stage has seen, quantized like the activations that leave the stage:
+ * one grid per token, head and side (key, value), code c of element x as in qp_quant_pack and its value as in
+ * qp_unpack_dequant.  For the head_dim elements x of a key or a value:
+ *     lo, hi    smallest and largest finite element, clamped to +-2^126 (0, 0 if none is finite)
+ *     scale     (hi - lo) / 15, or 0 if that is below 2^-120;   inv = 1 / scale, or 0    (fp32, correctly rounded)
+ *     c         rne((x - lo) * inv) clamped to [0, 15]          (fp32; +Inf -> 15, -Inf and NaN -> 0)
+ *     value     fma((float)c, scale, lo)
+ * Every grid in the cache is finite.
+ *
+ * Pages.  A page holds page_tokens tokens of all heads of one layer; the cache is layers x n_pages pages, page p of layer l
+ * at pages_dev + (l * n_pages + p) * qp_kv_page_bytes().  A page is kv_heads slabs of page_tokens * (head_dim + 16) bytes:
+ *     key codes     [page_tokens][head_dim / 8] words, code i of a word is element 8 w + i of the token (the wire format)
+ *     value codes   [page_tokens / 8][head_dim] words, code i of a word is token 8 g + i of the element
+ *     key grids     [page_tokens] {float lo, scale},  value grids [page_tokens] {float lo, scale}
+ * Value codes of eight tokens share a word because attention multiplies along the tokens there.
+ *
+ * Rows.  A row is a sequence: lengths_dev[r] tokens, token t in slot t mod page_tokens of page
+ * table_dev[r * pages_per_row + t div page_tokens].  The same pages serve all layers.  A page may belong to several rows
+ * (qp_kv_fork).  A table entry outside [0, n_pages) is a page that is not there: its tokens are not written, not attended to, and
+ * read as 0; a length is taken as at most pages_per_row * page_tokens and at least 0.  Nothing is read or written outside the
+ * cache whatever the table, the lengths and token_begin_dev hold.
+ *
+ * Tokens of a call.  token_begin_dev[0 .. rows] says which of the `tokens` tokens of the call's tensors belong to which row:
+ * row r has tokens token_begin_dev[r] .. token_begin_dev[r + 1] - 1 (ascending; cut off at 0 and `tokens`).  For qp_kv_append and
+ * qp_kv_attention they are the row's LAST tokens: lengths_dev counts them already, as qp_kv_reserve leaves it.  (Should a row
+ * have more of them than its length, the first ones have no place: they are not stored, and see nothing.)
+ *
+ * A step of a serving loop is qp_kv_reserve once, then qp_kv_append and qp_kv_attention for each layer.  All calls are
+ * asynchronous on `stream` and may be captured into a graph; results do not depend on the order of atomics.  Calls that touch
+ * the same rows or pages must be ordered by their streams, like any other writes to one buffer. */
+#define QP_KV_POOL_HEADER 16u   /* int32 words ahead of the reference counts in a pool record */
+typedef struct {
+    void    *pages_dev;        /* 16-byte aligned */
+    uint64_t pages_bytes;      /* >= layers * n_pages * qp_kv_page_bytes() */
+    uint32_t layers;           /* 1 .. 65536 */
+    uint32_t n_pages;          /* 1 .. 2^24 */
+    uint32_t kv_heads;         /* 1 .. 1024 */
+    uint32_t head_dim;         /* 64, 80, 96, 128 or 256 */
+    uint32_t page_tokens;      /* 32, 64, 128 or 256 */
+    uint32_t reserved;         /* 0 */
+} qp_kv_cache_t;
+typedef struct {
+    int32_t *table_dev;        /* [rows][pages_per_row] */
+    int32_t *lengths_dev;      /* [rows] */
+    uint32_t rows;             /* 1 .. 65536 */
+    uint32_t pages_per_row;    /* >= 1; pages_per_row * page_tokens < 2^31 */
+} qp_kv_rows_t;
+/* A tensor of `tokens` x heads x head_dim elements, the elements of a head next to each other.  16-byte aligned, strides multiples
+ * of 16 bytes; an input may have strides of 0 (a broadcast), an output's elements must not overlap. */
+typedef struct {
+    void    *data_dev;
+    uint32_t dtype;            /* qp_dtype */
+    uint32_t reserved;         /* 0 */
+    uint64_t token_stride;     /* in elements, < 2^40 */
+    uint64_t head_stride;
+} qp_kv_view_t;
+
+/* Bytes of one page of one layer: kv_heads * page_tokens * (head_dim + 16); 0 if the cache's sizes are refused. */
+size_t qp_kv_page_bytes(const qp_kv_cache_t *cache);
+
+/* ---- pages: handing out, sharing, freeing, moving together -----------------------------
+ * The pool record is int32 words in device memory: QP_KV_POOL_HEADER of header, then refs[n_pages], how many rows hold each page
+ * (0 = free), then room that the calls work in.  Header word 0: pages that the last qp_kv_reserve was short of (0: it was done);
+ * word 1: rows of the last qp_kv_reserve that would have outgrown pages_per_row; word 2: rows that the last qp_kv_fork
+ * refused; word 3: pages in use after the last qp_kv_compact.  qp_kv_pool_init makes every page free (do it once; it also clears
+ * the room that the calls need cleared between them, and they leave it so).  A row holds a page for each page_tokens
+ * tokens begun: a length of 0 is a row that holds none. */
+size_t qp_kv_pool_bytes(uint32_t n_pages);                     /* 4 * (16 + 6 n_pages); 0 if n_pages is refused */
+qp_status qp_kv_pool_init(uint32_t n_pages, void *pool_dev, size_t pool_bytes, void *stream);
+
+/* want_dev[r] more tokens for each row (0 or less: leave the row): gives it the pages for them and adds them to its length.
+ * A page that the row shares and would write into next is copied first, in all layers (copy on write).  As if one row after the other
+ * were served, each new page being the free one with the lowest index: the last holder of a shared page keeps it.  All or
+ * nothing: if pages are short or a row has not the table for it, no row is changed and header words 0 and 1 say so. */
+qp_status qp_kv_reserve(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, const int32_t *want_dev, void *pool_dev,
+                        size_t pool_bytes, void *stream);
+/* parent_dev[r] >= 0: row r, which must be empty, becomes a copy of row parent_dev[r] that shares its pages (nothing is copied
+ * until one of them grows).  A row that is not empty, is its own parent, or names a parent that is out of range or is itself forked
+ * in this call is left as it is and counted in header word 2. */
+qp_status qp_kv_fork(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, const int32_t *parent_dev, void *pool_dev,
+                     size_t pool_bytes, void *stream);
+/* keep_dev[r] >= 0: row r keeps its first keep_dev[r] tokens (0: none, the row is freed; drafted tokens that were rejected go the same
+ * way) and gives up the pages behind them; a negative value leaves the row.  Entries given up become -1. */
+qp_status qp_kv_free(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, const int32_t *keep_dev, void *pool_dev,
+                     size_t pool_bytes, void *stream);
+/* Moves the pages in use together: with L of them, the i-th page in use at or above L goes to the i-th free place below L (both in
+ * ascending order), in all layers, and the rows' tables follow.  `rows` must be all rows that hold pages of the pool. */
+qp_status qp_kv_compact(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, void *pool_dev, size_t pool_bytes, void *stream);
+
+/* ---- rows in and out -------------------------------------------------------------------
+ * qp_kv_append quantizes the call's tokens into the pages of one layer (a page that several rows hold is theirs together: reserve
+ * first).  qp_kv_read writes tokens first_dev[r], first_dev[r] + 1, ... of each row (first_dev NULL: from 0) to k and v,
+ * in the views' types (fp32 values rounded once for QP_BF16); tokens at or behind the row's length read as 0, and elements of k
+ * and v that belong to no row stay as they are.  k and v are of one type; tokens == 0 does nothing. */
+qp_status qp_kv_append(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, uint32_t layer, const int32_t *token_begin_dev,
+                       uint64_t tokens, const qp_kv_view_t *k, const qp_kv_view_t *v, void *stream);
+qp_status qp_kv_read(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, uint32_t layer, const int32_t *token_begin_dev,
+                     const int32_t *first_dev, uint64_t tokens, const qp_kv_view_t *k, const qp_kv_view_t *v, void *stream);
+
+/* ---- attention over the cache ----------------------------------------------------------
+ * out = softmax(scale * q K^T) V for each of the call's tokens and each of q_heads query heads; query head h goes with key head
+ * h div (q_heads / kv_heads).  causal: token i of a row's m, at position p = length - m + i, sees tokens t <= p, and with window > 0
+ * only t > p - window; without causal it sees the whole row (window must be 0).  A query that sees nothing gives 0; one
+ * that holds NaN or Inf gives NaN, and no other query does.  Dot products of codes and queries are exact, sums and softmax are fp32;
+ * out has q's type.  Long rows are split among blocks and joined in a fixed order: results are the same on every run.
+ * The workspace needs no initialisation. */
+typedef struct {
+    float    scale;            /* > 0, finite */
+    uint32_t q_heads;          /* a multiple of kv_heads, at most 1024 times it */
+    uint32_t causal;           /* 0 or 1 */
+    uint32_t window;           /* 0 = none; < 2^31 */
+} qp_kv_attn_cfg_t;
+size_t qp_kv_attention_workspace_bytes(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, uint64_t tokens, uint32_t q_heads);
+qp_status qp_kv_attention(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, uint32_t layer, const int32_t *token_begin_dev,
+                          uint64_t tokens, const qp_kv_view_t *q, const qp_kv_view_t *out, const qp_kv_attn_cfg_t *cfg,
+                          void *ws_dev, size_t ws_bytes, void *stream);
+
 const char *qp_strerror(qp_status status);
 
 #ifdef __cplusplus

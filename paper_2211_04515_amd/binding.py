@@ -19,7 +19,11 @@ __all__ = [
     "lib", "qp_packed_bytes", "qp_workspace_bytes", "qp_ws_offset", "qp_default_search_cfg", "qp_stats",
     "qp_stats_async", "qp_aciq_alpha", "qp_aciq_constant", "qp_make_qparams", "qp_make_qparams_clipped", "qp_dsaciq_search",
     "qp_dsaciq_search_async", "qp_dsaciq_hist_search", "qp_dsaciq_hist_search_async", "qp_quant_pack", "qp_quant_pack_dev", "qp_unpack_dequant", "qp_unpack_dequant_dev",
-    "qp_compress_async", "qp_compress_many_async", "qp_compress_noalloc", "qp_next_bits", "qp_controller_init", "qp_controller_update", "qp_strerror", "alloc_workspace", "alloc_packed", "dtype_of", "read_ws",
+    "qp_compress_async", "qp_compress_many_async", "qp_compress_noalloc", "qp_next_bits", "qp_controller_init", "qp_controller_update", "qp_strerror",
+    "QP_KV_POOL_HEADER", "qp_kv_cache_t", "qp_kv_rows_t", "qp_kv_view_t", "qp_kv_attn_cfg_t", "kv_cache", "kv_rows", "alloc_kv_pages", "alloc_kv_pool", "alloc_kv_workspace",
+    "qp_kv_page_bytes", "qp_kv_pool_bytes", "qp_kv_pool_init", "qp_kv_reserve", "qp_kv_fork", "qp_kv_free", "qp_kv_compact", "qp_kv_append", "qp_kv_read",
+    "qp_kv_attention_workspace_bytes", "qp_kv_attention",
+    "alloc_workspace", "alloc_packed", "dtype_of", "read_ws",
 ]
 
 QP_OK, QP_EINVAL, QP_ENOSPC, QP_EHIP, QP_ENONFINITE = 0, -1, -2, -3, -4
@@ -28,6 +32,8 @@ QP_LAPLACE, QP_GAUSS, QP_DIST_AUTO = 0, 1, 2
 QP_SEARCH_CLIP_TO_DATA, QP_SEARCH_COARSE_TO_FINE, QP_SEARCH_LOW_BITS_ONLY = 1, 2, 4
 QP_WS_STATS, QP_WS_RESULT, QP_WS_QPARAMS, QP_WS_HIST, QP_WS_CANDS, QP_WS_SCORES, QP_WS_MODEL = range(7)
 BITS = (2, 3, 4, 6, 8, 16)
+
+QP_KV_POOL_HEADER = 16   # int32 words ahead of the reference counts in a pool record
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libquantpipe.so")
 
@@ -71,6 +77,24 @@ class qp_job_t(C.Structure):
 
 class qp_lane_t(C.Structure):
     _fields_ = [("ws_dev", C.c_void_p), ("ws_bytes", C.c_size_t), ("stream", C.c_void_p)]
+
+
+class qp_kv_cache_t(C.Structure):
+    _fields_ = [("pages_dev", C.c_void_p), ("pages_bytes", C.c_uint64), ("layers", C.c_uint32), ("n_pages", C.c_uint32),
+                ("kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("page_tokens", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class qp_kv_rows_t(C.Structure):
+    _fields_ = [("table_dev", C.c_void_p), ("lengths_dev", C.c_void_p), ("rows", C.c_uint32), ("pages_per_row", C.c_uint32)]
+
+
+class qp_kv_view_t(C.Structure):
+    _fields_ = [("data_dev", C.c_void_p), ("dtype", C.c_uint32), ("reserved", C.c_uint32), ("token_stride", C.c_uint64),
+                ("head_stride", C.c_uint64)]
+
+
+class qp_kv_attn_cfg_t(C.Structure):
+    _fields_ = [("scale", C.c_float), ("q_heads", C.c_uint32), ("causal", C.c_uint32), ("window", C.c_uint32)]
 
 
 class QuantPipeError(RuntimeError):
@@ -121,6 +145,17 @@ def lib():
             "qp_next_bits": (i32, [C.c_double, u32, C.c_double, C.c_double, C.c_double, C.POINTER(u32)]),
             "qp_controller_init": (i32, [C.POINTER(qp_controller_t), u32, C.c_double, C.c_double, u32]),
             "qp_controller_update": (i32, [C.POINTER(qp_controller_t), C.c_double, C.c_double, C.POINTER(u32)]),
+            "qp_kv_page_bytes": (sz, [vp]),
+            "qp_kv_pool_bytes": (sz, [u32]),
+            "qp_kv_pool_init": (i32, [u32, vp, sz, vp]),
+            "qp_kv_reserve": (i32, [vp, vp, vp, vp, sz, vp]),
+            "qp_kv_fork": (i32, [vp, vp, vp, vp, sz, vp]),
+            "qp_kv_free": (i32, [vp, vp, vp, vp, sz, vp]),
+            "qp_kv_compact": (i32, [vp, vp, vp, sz, vp]),
+            "qp_kv_append": (i32, [vp, vp, u32, vp, u64, vp, vp, vp]),
+            "qp_kv_read": (i32, [vp, vp, u32, vp, vp, u64, vp, vp, vp]),
+            "qp_kv_attention_workspace_bytes": (sz, [vp, vp, u64, u32]),
+            "qp_kv_attention": (i32, [vp, vp, u32, vp, u64, vp, vp, vp, vp, sz, vp]),
             "qp_strerror": (C.c_char_p, [i32]),
         }
         for name, (res, args) in sig.items():
@@ -135,6 +170,8 @@ EXPORTS = ("qp_packed_bytes", "qp_workspace_bytes", "qp_ws_offset", "qp_default_
            "qp_stats_async", "qp_aciq_alpha", "qp_aciq_constant", "qp_make_qparams", "qp_make_qparams_clipped", "qp_dsaciq_search",
            "qp_dsaciq_search_async", "qp_model_fit", "qp_model_fit_async", "qp_dsaciq_hist_search", "qp_dsaciq_hist_search_async", "qp_quant_pack", "qp_quant_pack_dev", "qp_unpack_dequant",
            "qp_unpack_dequant_dev", "qp_compress_async", "qp_compress_many_async", "qp_compress_noalloc", "qp_next_bits", "qp_controller_init", "qp_controller_update",
+           "qp_kv_page_bytes", "qp_kv_pool_bytes", "qp_kv_pool_init", "qp_kv_reserve", "qp_kv_fork", "qp_kv_free", "qp_kv_compact",
+           "qp_kv_append", "qp_kv_read", "qp_kv_attention_workspace_bytes", "qp_kv_attention",
            "qp_strerror")
 
 
@@ -356,3 +393,160 @@ def qp_dsaciq_hist_search(bits: int, ws, cfg=None, stream=None):
 def qp_dsaciq_hist_search_async(bits: int, ws, cfg=None, stream=None) -> None:
     _check(lib().qp_dsaciq_hist_search_async(int(bits), _cfgp(cfg), _dev(ws), ws.numel(), _stream(stream)),
            "qp_dsaciq_hist_search_async")
+
+
+# ---- the key/value cache in 4 bits ----------------------------------------------------------
+# The structs hold device addresses; the tensors behind them are kept alive by the struct objects (`tensors`).  Tensors of a call
+# lie on one device; a call goes to that device's current stream (or to `stream`, which must be one of its streams).
+
+def kv_cache(pages, kv_heads: int, head_dim: int, page_tokens: int) -> qp_kv_cache_t:
+    """The cache in `pages`: contiguous device bytes of shape [layers, n_pages, ...] (alloc_kv_pages makes them)."""
+    if pages.dim() < 2 or pages.dtype != torch.uint8 or not pages.is_contiguous() or not pages.is_cuda:
+        raise ValueError("pages: expected a contiguous uint8 device tensor [layers, n_pages, ...]")
+    c = qp_kv_cache_t(pages.data_ptr(), pages.numel(), pages.shape[0], pages.shape[1], kv_heads, head_dim, page_tokens, 0)
+    if qp_kv_page_bytes(c) == 0:
+        raise QuantPipeError(QP_EINVAL, "kv_cache")
+    c.tensors = (pages,)
+    return c
+
+
+def kv_rows(table, lengths) -> qp_kv_rows_t:
+    """Rows with their page table, int32 [rows, pages_per_row], and lengths, int32 [rows]."""
+    if table.dim() != 2 or tuple(lengths.shape) != (table.shape[0],):
+        raise ValueError("expected table [rows, pages_per_row] and lengths [rows]")
+    r = qp_kv_rows_t(_ints(table, table.numel(), table.device), _ints(lengths, table.shape[0], table.device), table.shape[0], table.shape[1])
+    r.tensors = (table, lengths)
+    return r
+
+
+def alloc_kv_pages(n_pages: int, kv_heads: int, head_dim: int, page_tokens: int, layers: int = 1, device="cuda") -> "torch.Tensor":
+    """Room for a cache, not initialised: what was never written is never looked at."""
+    nb = qp_kv_page_bytes(qp_kv_cache_t(None, 0, layers, n_pages, kv_heads, head_dim, page_tokens, 0))
+    if nb == 0:
+        raise QuantPipeError(QP_EINVAL, "qp_kv_page_bytes")
+    return torch.empty((layers, n_pages, kv_heads, nb // kv_heads), dtype=torch.uint8, device=device)
+
+
+def alloc_kv_pool(n_pages: int, device="cuda") -> "torch.Tensor":
+    """A pool record with every page free: int32, the header, then the reference counts refs[n_pages], then room."""
+    nb = qp_kv_pool_bytes(n_pages)
+    if nb == 0:
+        raise QuantPipeError(QP_EINVAL, "qp_kv_pool_bytes")
+    pool = torch.empty(nb // 4, dtype=torch.int32, device=device)
+    qp_kv_pool_init(n_pages, pool)
+    return pool
+
+
+def alloc_kv_workspace(cache: qp_kv_cache_t, rows: qp_kv_rows_t, tokens: int, q_heads: int) -> "torch.Tensor":
+    nb = qp_kv_attention_workspace_bytes(cache, rows, tokens, q_heads)
+    if nb == 0:
+        raise QuantPipeError(QP_EINVAL, "qp_kv_attention_workspace_bytes")
+    return torch.empty(nb, dtype=torch.uint8, device=cache.tensors[0].device)
+
+
+def _ints(t, count: int, device):
+    if t.dtype != torch.int32 or t.numel() < count or not t.is_contiguous() or not t.is_cuda or t.device != device:
+        raise ValueError("expected a contiguous int32 tensor of at least %d entries on %s" % (count, device))
+    return t.data_ptr()
+
+
+def _view(t, heads: int, dim: int, tokens: int, device) -> qp_kv_view_t:
+    if t.dim() != 3 or t.shape[0] != tokens or t.shape[1] != heads or t.shape[2] != dim or t.device != device:
+        raise ValueError("expected a tensor [%d, %d, %d] on %s, got %s on %s" % (tokens, heads, dim, device, tuple(t.shape), t.device))
+    s = t.stride()
+    if s[2] != 1:
+        raise ValueError("the elements of a head must lie next to each other")
+    # (an axis of one entry may carry any stride: it is never used)
+    return qp_kv_view_t(t.data_ptr(), dtype_of(t), 0, s[0] if tokens > 1 else 0, s[1] if heads > 1 else 0)
+
+
+def _kv_call(device, stream, what: str, *args) -> None:
+    """The library's call on the device's own current stream, with that device current (kernels go to the current one)."""
+    if device.index == torch.cuda.current_device():
+        st = getattr(lib(), what)(*args, C.c_void_p((torch.cuda.current_stream() if stream is None else stream).cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            st = getattr(lib(), what)(*args, C.c_void_p((torch.cuda.current_stream() if stream is None else stream).cuda_stream))
+    _check(st, what)
+
+
+def qp_kv_page_bytes(cache: qp_kv_cache_t) -> int:
+    return int(lib().qp_kv_page_bytes(C.byref(cache)))
+
+
+def qp_kv_pool_bytes(n_pages: int) -> int:
+    return int(lib().qp_kv_pool_bytes(int(n_pages)))
+
+
+def qp_kv_attention_workspace_bytes(cache: qp_kv_cache_t, rows: qp_kv_rows_t, tokens: int, q_heads: int) -> int:
+    return int(lib().qp_kv_attention_workspace_bytes(C.byref(cache), C.byref(rows), int(tokens), int(q_heads)))
+
+
+def qp_kv_pool_init(n_pages: int, pool, stream=None) -> None:
+    _kv_call(pool.device, stream, "qp_kv_pool_init", int(n_pages), _ints(pool, 1, pool.device), pool.numel() * 4)
+
+
+def _books(what: str, cache, rows, pool, per_row, stream) -> None:
+    d = cache.tensors[0].device
+    _same_device(d, rows)
+    _kv_call(d, stream, what, C.byref(cache), C.byref(rows), _ints(per_row, rows.rows, d), _ints(pool, 1, d), pool.numel() * 4)
+
+
+def _same_device(device, rows) -> None:
+    if rows.tensors[0].device != device:
+        raise ValueError("the rows are on %s, the pages on %s" % (rows.tensors[0].device, device))
+
+
+def qp_kv_reserve(cache, rows, pool, want, stream=None) -> None:
+    """want[r] more tokens for each row; words 0 and 1 of `pool` say afterwards whether it was done (both 0) or nothing was."""
+    _books("qp_kv_reserve", cache, rows, pool, want, stream)
+
+
+def qp_kv_fork(cache, rows, pool, parent, stream=None) -> None:
+    """Row r becomes a copy of row parent[r] (negative: left alone) that shares its pages; word 2 of `pool` counts refused rows."""
+    _books("qp_kv_fork", cache, rows, pool, parent, stream)
+
+
+def qp_kv_free(cache, rows, pool, keep, stream=None) -> None:
+    """Row r keeps its first keep[r] tokens (negative: left alone) and gives up the pages behind them."""
+    _books("qp_kv_free", cache, rows, pool, keep, stream)
+
+
+def qp_kv_compact(cache, rows, pool, stream=None) -> None:
+    """Moves the pages in use to the pool's low end; word 3 of `pool` says how many there are."""
+    d = cache.tensors[0].device
+    _same_device(d, rows)
+    _kv_call(d, stream, "qp_kv_compact", C.byref(cache), C.byref(rows), _ints(pool, 1, d), pool.numel() * 4)
+
+
+def qp_kv_append(cache, rows, layer: int, token_begin, k, v, stream=None) -> None:
+    """Quantizes k, v [tokens, kv_heads, head_dim] into the rows' last places."""
+    d = cache.tensors[0].device
+    _same_device(d, rows)
+    n = k.shape[0]
+    kv, vv = _view(k, cache.kv_heads, cache.head_dim, n, d), _view(v, cache.kv_heads, cache.head_dim, n, d)
+    _kv_call(d, stream, "qp_kv_append", C.byref(cache), C.byref(rows), int(layer), _ints(token_begin, rows.rows + 1, d), n, C.byref(kv), C.byref(vv))
+
+
+def qp_kv_read(cache, rows, layer: int, token_begin, k, v, first=None, stream=None) -> None:
+    """Writes the rows' tokens from first[r] (None: 0) on to k, v [tokens, kv_heads, head_dim]."""
+    d = cache.tensors[0].device
+    _same_device(d, rows)
+    n = k.shape[0]
+    kv, vv = _view(k, cache.kv_heads, cache.head_dim, n, d), _view(v, cache.kv_heads, cache.head_dim, n, d)
+    f = None if first is None else _ints(first, rows.rows, d)
+    _kv_call(d, stream, "qp_kv_read", C.byref(cache), C.byref(rows), int(layer), _ints(token_begin, rows.rows + 1, d), f, n, C.byref(kv), C.byref(vv))
+
+
+def qp_kv_attention(cache, rows, layer: int, token_begin, q, out, ws, scale: float = None, causal: bool = True, window: int = 0,
+                    stream=None) -> None:
+    """out = softmax(scale q K^T) V for the rows' last tokens; q, out [tokens, q_heads, head_dim]; scale None: 1 / sqrt(head_dim)."""
+    d = cache.tensors[0].device
+    _same_device(d, rows)
+    n, heads = q.shape[0], q.shape[1]
+    qv, ov = _view(q, heads, cache.head_dim, n, d), _view(out, heads, cache.head_dim, n, d)
+    if ws.device != d or not ws.is_contiguous():
+        raise ValueError("expected a contiguous workspace on %s" % d)
+    cfg = qp_kv_attn_cfg_t(cache.head_dim ** -0.5 if scale is None else scale, heads, 1 if causal else 0, int(window))
+    _kv_call(d, stream, "qp_kv_attention", C.byref(cache), C.byref(rows), int(layer), _ints(token_begin, rows.rows + 1, d), n, C.byref(qv), C.byref(ov),
+             C.byref(cfg), ws.data_ptr(), ws.numel() * ws.element_size())

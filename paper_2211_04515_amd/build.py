@@ -1,4 +1,4 @@
-"""Compile the HIP library (csrc/*.hip) for gfx950 into libquantpipe.so next to this file."""
+"""Compile the HIP library (csrc/*.hip, csrc/kv/*.hip) for gfx950 into libquantpipe.so next to this file."""
 from __future__ import annotations
 
 import glob
@@ -30,7 +30,7 @@ def _compile(src: str) -> str:
 
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
-    srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
+    srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "kv", "*.hip")))
     with ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
         objs = list(ex.map(_compile, srcs))
     subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs], check=True)
