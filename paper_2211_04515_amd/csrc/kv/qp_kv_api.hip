@@ -51,7 +51,7 @@ qp_status check_rows(const qp_kv_cache_t *c, const qp_kv_rows_t *r)
 }
 qp_status check_pool(uint32_t n_pages, const void *pool, size_t bytes)
 {
-    if (!pool || !aligned16(pool)) return QP_EINVAL;
+    if (!pool || !aligned4(pool)) return QP_EINVAL;
     return bytes >= qp_kv_pool_bytes(n_pages) ? QP_OK : QP_ENOSPC;
 }
 // What reserve, fork, free and compact have in common.

@@ -44,6 +44,11 @@ constexpr uint32_t kAtTile = kAtStep * kAtWaves; // tokens that work is counted 
 #endif
 // pieces that a call is cut into: what the chip runs at the same time
 template <int NCT> constexpr uint32_t kAtTarget = NCT == 1 ? QP_KV_TARGET : QP_KV_TARGET / 2;
+// tiles that a piece has at least: joining costs a kernel and a pass over the pieces, more than it takes to go through these
+#ifndef QP_KV_LEAST
+#define QP_KV_LEAST 4
+#endif
+constexpr uint32_t kAtLeast = QP_KV_LEAST;
 constexpr float kAtHeadroom = 8.0f;              // log2 that a score may lie above its column's m
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -69,8 +74,10 @@ template <int NCT> AtWork at_work(void *ws, const KvLayer &c, uint32_t dim, uint
 {
     const uint64_t tiles = (((uint64_t)c.pages_per_row << c.page_shift) + kAtTile - 1u) / kAtTile, items = at_items(NCT, c, group);
     const uint64_t columns = (uint64_t)c.tokens * c.kv_heads * group, target = kAtTarget<NCT>;
-    uint64_t pieces = tiles < 2u ? 0u : 2u * target, cols = tiles < 2u ? 0u : target * 64u * NCT;
-    if (items < 2u * target && items * tiles < pieces) pieces = items * tiles;
+    // a piece's share is at least kAtLeast tiles, a quarter of them where the waves split columns
+    const uint64_t least = (uint64_t)c.tokens * group > 16u * NCT ? (kAtLeast + 3u) / 4u : kAtLeast;
+    uint64_t pieces = tiles <= least ? 0u : 2u * target, cols = tiles <= least ? 0u : target * 64u * NCT;
+    if (items < 2u * target && items * tiles < pieces) pieces = items * tiles;   // (one tile each at the least)
     if (columns < cols) cols = columns;
     AtWork w{};
     w.most_units = (uint32_t)(pieces * ((uint64_t)c.tokens * group > 16u * NCT ? 4u : 1u));
@@ -109,69 +116,78 @@ struct AtPiece {
     uint32_t unit, unit_step;                // where the item's partial results go (piece s at unit + s unit_step)
     uint32_t col;                            // ... and its columns' records
 };
-__device__ __forceinline__ uint32_t at_scan(uint32_t v, uint32_t *part, uint32_t &total)
+// Inclusive prefix sums of three numbers over the block; `part` holds each wave's totals.
+__device__ __forceinline__ void at_scan(uint32_t (&x)[3], uint32_t (*part)[3], uint32_t (&total)[3])
 {
     const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    uint32_t x = v;
 #pragma unroll
-    for (uint32_t d = 1; d < (uint32_t)kWave; d *= 2u) {
-        const uint32_t o = __shfl_up(x, d, kWave);
-        if (lane >= d) x += o;
-    }
-    if (lane == kWave - 1u) part[wave] = x;
+    for (uint32_t d = 1; d < (uint32_t)kWave; d *= 2u)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const uint32_t o = __shfl_up(x[i], d, kWave);
+            if (lane >= d) x[i] += o;
+        }
+    if (lane == kWave - 1u)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) part[wave][i] = x[i];
     __syncthreads();
-    uint32_t before = 0;
-    total = 0;
 #pragma unroll
-    for (uint32_t w = 0; w < (uint32_t)kAtWaves; ++w) {
-        before += w < wave ? part[w] : 0u;
-        total += part[w];
+    for (int i = 0; i < 3; ++i) {
+        total[i] = 0u;
+#pragma unroll
+        for (uint32_t w = 0; w < (uint32_t)kAtWaves; ++w) {
+            x[i] += w < wave ? part[w][i] : 0u;
+            total[i] += part[w][i];
+        }
     }
-    return x + before;
+}
+__device__ __forceinline__ uint64_t at_wave_sum(uint64_t v)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) v += ((uint64_t)__shfl_xor((uint32_t)(v >> 32), d, kWave) << 32) + __shfl_xor((uint32_t)v, d, kWave);
+    return v;
 }
 
 // False: the call has fewer pieces than blocks.
 template <int NCT>
 __device__ __forceinline__ bool at_find(const KvLayer &c, const KvAttn &a, const AtWork &w, uint32_t block, AtPiece &mine)
 {
-    __shared__ uint32_t part[3][kAtWaves];
-    __shared__ unsigned long long work;
+    __shared__ uint32_t part[kAtWaves][3];
+    __shared__ uint64_t work[kAtWaves];
     __shared__ AtPiece found;
     __shared__ uint32_t have, split;
     const uint32_t tid = threadIdx.x;
-    if (tid == 0u) {
-        work = 0ull;
-        have = split = 0u;
-    }
-    __syncthreads();
-    uint64_t cost = 0;
-    for (uint32_t r = tid; r < c.rows; r += kAtThreads) {
+    const AtRow none{0u, 0u, 1u, 0u};
+    const AtRow mine0 = tid < c.rows ? at_row<NCT>(c, a, tid) : none;      // (most calls have no more rows than that)
+    uint64_t cost = (uint64_t)mine0.tiles * (mine0.n4 * 4u + mine0.n1);
+    for (uint32_t r = tid + kAtThreads; r < c.rows; r += kAtThreads) {
         const AtRow o = at_row<NCT>(c, a, r);
         cost += (uint64_t)o.tiles * (o.n4 * 4u + o.n1);
     }
-    if (cost != 0u) atomicAdd(&work, (unsigned long long)cost);
+    cost = at_wave_sum(cost);
+    if (tid % kWave == 0u) work[tid / kWave] = cost;
+    if (tid == 0u) have = split = 0u;
     __syncthreads();
-    const uint64_t all = (uint64_t)work * c.kv_heads;
-    const uint64_t share = max((all + kAtTarget<NCT> - 1u) / kAtTarget<NCT>, (uint64_t)1u);
+    const uint64_t all = (work[0] + work[1] + work[2] + work[3]) * c.kv_heads;
+    const uint64_t share = max((all + kAtTarget<NCT> - 1u) / kAtTarget<NCT>, (uint64_t)kAtLeast);
     const uint32_t per1 = (uint32_t)min(share, (uint64_t)0x7fffffffu), per4 = (uint32_t)min((share + 3u) / 4u, (uint64_t)0x7fffffffu);
-    uint32_t blocks = 0, units = 0, cols = 0;
+    uint32_t before[3] = {0u, 0u, 0u};                   // blocks, units, columns of the rows so far
     for (uint32_t r0 = 0; r0 < c.rows; r0 += kAtThreads) {
         const uint32_t r = r0 + tid;
-        const AtRow o = r < c.rows ? at_row<NCT>(c, a, r) : AtRow{0u, 0u, 1u, 0u};
+        const AtRow o = r0 == 0u ? mine0 : r < c.rows ? at_row<NCT>(c, a, r) : none;
         const uint32_t s4 = (o.tiles + per4 - 1u) / per4, s1 = (o.tiles + per1 - 1u) / per1;
         const uint32_t last = o.n1 ? o.cols - o.n4 * 64u * NCT : 0u;          // columns of the item with split tokens
         const uint32_t b4 = c.kv_heads * o.n4 * s4, b1 = c.kv_heads * o.n1 * s1;
         const uint32_t u4 = s4 > 1u ? 4u * b4 : 0u, u1 = s1 > 1u ? b1 : 0u;
         const uint32_t k4 = s4 > 1u ? c.kv_heads * (o.cols - last) : 0u, k1 = s1 > 1u ? c.kv_heads * last : 0u;
-        uint32_t tb, tu, tk;
-        const uint32_t pb = blocks + at_scan(b4 + b1, part[0], tb) - (b4 + b1);
-        const uint32_t pu = units + at_scan(u4 + u1, part[1], tu) - (u4 + u1);
-        const uint32_t pk = cols + at_scan(k4 + k1, part[2], tk) - (k4 + k1);
+        uint32_t x[3] = {b4 + b1, u4 + u1, k4 + k1}, total[3];
+        at_scan(x, part, total);
+        const uint32_t eb = before[0] + x[0], eu = before[1] + x[1], ek = before[2] + x[2];      // ends
+        const uint32_t pb = eb - (b4 + b1), pu = eu - (u4 + u1), pk = ek - (k4 + k1);
         // (always so where the rows' tokens do not overlap: what the host sized the grid and the workspace for)
-        const bool fits = pb <= gridDim.x && pb + b4 + b1 <= gridDim.x && pu <= w.most_units && pu + u4 + u1 <= w.most_units &&
-                          pk <= w.most_cols && pk + k4 + k1 <= w.most_cols;
-        if (fits && k4 + k1 != 0u) atomicMax(&split, pk + k4 + k1);
-        if (fits && block >= pb && block < pb + b4 + b1) {
+        const bool fits = pb <= gridDim.x && eb <= gridDim.x && pu <= w.most_units && eu <= w.most_units && pk <= w.most_cols && ek <= w.most_cols;
+        if (fits && k4 + k1 != 0u) atomicMax(&split, ek);
+        if (fits && block >= pb && block < eb) {
             uint32_t i = block - pb;
             AtPiece f;
             f.row = r;
@@ -199,11 +215,10 @@ __device__ __forceinline__ bool at_find(const KvLayer &c, const KvAttn &a, const
             found = f;
             have = 1u;
         }
-        blocks += tb;
-        units += tu;
-        cols += tk;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) before[k] += total[k];
         __syncthreads();
-        if (block < blocks && block != 0u) break;    // (block 0 goes on: it says how many columns were split)
+        if (block < before[0] && block != 0u) break;     // (block 0 goes on: it says how many columns were split)
     }
     if (block == 0u && tid == 0u) w.header[0] = split;
     mine = found;
@@ -211,14 +226,25 @@ __device__ __forceinline__ bool at_find(const KvLayer &c, const KvAttn &a, const
 }
 
 // ---- a wave's work -----------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ f16x8 at_codes(uint32_t w)
+// The constants of at_codes in vector registers: (w & mask) | magic is one instruction then (it takes one scalar operand only),
+// and two with the constants in it.
+struct AtMagic {
+    uint32_t big, small;
+    __device__ __forceinline__ AtMagic() : big(0x64006400u), small(0x54005400u)
+    {
+#if defined(__AMDGCN__)
+        asm volatile("" : "+v"(big), "+v"(small));
+#endif
+    }
+};
+__device__ __forceinline__ f16x8 at_codes(uint32_t w, const AtMagic &k)
 {
     const f16x2 big = {(_Float16)-1032.0f, (_Float16)-1032.0f}, small = {(_Float16)-72.0f, (_Float16)-72.0f};
     const uint32_t x = w >> 8;
-    const f16x2 a = __builtin_bit_cast(f16x2, (w & 0x000f000fu) | 0x64006400u) + big;
-    const f16x2 b = __builtin_bit_cast(f16x2, (w & 0x00f000f0u) | 0x54005400u) + small;
-    const f16x2 d = __builtin_bit_cast(f16x2, (x & 0x000f000fu) | 0x64006400u) + big;
-    const f16x2 e = __builtin_bit_cast(f16x2, (x & 0x00f000f0u) | 0x54005400u) + small;
+    const f16x2 a = __builtin_bit_cast(f16x2, (w & 0x000f000fu) | k.big) + big;
+    const f16x2 b = __builtin_bit_cast(f16x2, (w & 0x00f000f0u) | k.small) + small;
+    const f16x2 d = __builtin_bit_cast(f16x2, (x & 0x000f000fu) | k.big) + big;
+    const f16x2 e = __builtin_bit_cast(f16x2, (x & 0x00f000f0u) | k.small) + small;
     return f16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
 }
 __device__ __forceinline__ float at_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -301,8 +327,9 @@ template <int D, int NCT, int DT> struct AtWave {
             sum += kv_xor_f32(sum, 16);
             sum += kv_xor_f32(sum, 32);
             bq[t] = any ? __uint_as_float(0x7fc00000u) : sum;
-            f[t] = ldexpf(a.scale * 1.44269504088896341f, -up);
-            m[t] = -3.402823466e38f;
+            // f > 0, and m f finite from the start: a masked score, -inf, gives p = 0 by itself
+            f[t] = fmaxf(ldexpf(a.scale * 1.44269504088896341f, -up), 0x1p-126f);
+            m[t] = -0x1p127f / fmaxf(f[t], 1.0f);
             l[t] = lv[t] = 0.0f;
 #pragma unroll
             for (int b = 0; b < NB; ++b) o[t][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -332,8 +359,7 @@ template <int D, int NCT, int DT> struct AtWave {
     }
 
     // the maximum or N moves
-    __device__ __noinline__ void rescale(const float (&top)[NCT], float sv_top) { rescale_inline(top, sv_top); }
-    __device__ __forceinline__ void rescale_inline(const float (&top)[NCT], float sv_top)
+    __device__ __forceinline__ void rescale(const float (&top)[NCT], float sv_top)
     {
         sv_top = fmaxf(sv_top, kv_xor_f32(sv_top, 16));
         sv_top = fmaxf(sv_top, kv_xor_f32(sv_top, 32));
@@ -362,24 +388,23 @@ template <int D, int NCT, int DT> struct AtWave {
         }
     }
 
-    // `mem`: 32 keys' and 32 values' grids, this wave's own
-    __device__ __forceinline__ void step(const Raw &x, float2 *mem, uint32_t t0, bool whole, bool there)
+    // What a step makes of a grid; lanes 0..31: keys, 32..63: values.
+    static __device__ __forceinline__ float2 centred(float2 grid) { return float2{grid.y, fmaf(8.0f, grid.y, grid.x)}; }
+
+    // `key(j, k)`, `value(b)`: the fragments; `mem`: scales and lo + 8 scale of 32 keys, then of 32 values
+    template <typename Key, typename Value>
+    __device__ __forceinline__ void step(const Key &key, const Value &value, const float2 *mem, uint32_t t0, bool whole, bool there)
     {
         const uint32_t lane = threadIdx.x % kWave, g = lane / 16u;
-        mem[lane] = x.grid;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        float sk[8], bk[8], sv[8], bv[8];                 // of tokens 8 g + i: scales and lo + 8 scale
+        float sk[8], bk[8], sv[8], bv[8];                 // of tokens 8 g + i
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float2 gk = mem[8u * g + i], gv = mem[32u + 8u * g + i];
-            sk[i] = gk.y;
-            bk[i] = fmaf(8.0f, gk.y, gk.x);
-            sv[i] = gv.y;
-            bv[i] = fmaf(8.0f, gv.y, gv.x);
+            sk[i] = gk.x;
+            bk[i] = gk.y;
+            sv[i] = gv.x;
+            bv[i] = gv.y;
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
         f32x4 s[NCT][2];
 #pragma unroll
         for (int t = 0; t < NCT; ++t) s[t][0] = s[t][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -387,33 +412,38 @@ template <int D, int NCT, int DT> struct AtWave {
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const f16x8 a = at_codes(x.k[j][k]);
+                const f16x8 a = key(j, k);
 #pragma unroll
                 for (int t = 0; t < NCT; ++t)
 #pragma unroll
-                    for (int z = 0; z < PIECES; ++z) s[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, q[t][z][k], s[t][j], 0, 0, 0);
+                    for (int z = PIECES - 1; z >= 0; --z) s[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, q[t][z][k], s[t][j], 0, 0, 0);
             }
         float y[NCT][8], top[NCT];
-        bool moves = false;
         float sv_top = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) sv_top = fmaxf(sv_top, sv[i]);
-        moves |= sv_top > sv_most;
+        bool moves = sv_top > sv_most;
 #pragma unroll
         for (int t = 0; t < NCT; ++t) {
-            top[t] = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                y[t][i] = fmaf(s[t][i / 4][i % 4], sk[i], bk[i] * bq[t]);
-                if (!whole) {
-                    const int32_t tok = (int32_t)(t0 + 8u * g + i);
+            for (int i = 0; i < 8; ++i) y[t][i] = fmaf(s[t][i / 4][i % 4], sk[i], bk[i] * bq[t]);
+            if (!whole) {
+                uint32_t from = t0 + 8u * g;
+#if defined(__AMDGCN__)
+                asm volatile("" : "+v"(from));   // (keeps this inside the branch: else 24 instructions of it are in every step)
+#endif
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int32_t tok = (int32_t)from + i;
                     if (!there || tok < lo[t] || tok >= hi[t]) y[t][i] = -INFINITY;
                 }
-                top[t] = fmaxf(top[t], y[t][i]);
             }
+            top[t] = y[t][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top[t] = fmaxf(top[t], y[t][i]);
             moves |= (top[t] - m[t]) * f[t] > kAtHeadroom;
         }
-        if (__ballot(moves) != 0ull) rescale_inline(top, sv_top);
+        if (__ballot(moves) != 0ull) rescale(top, sv_top);
         f16x8 p[NCT][PIECES];
 #pragma unroll
         for (int i = 0; i < 8; ++i) sv[i] *= norm;
@@ -422,8 +452,7 @@ template <int D, int NCT, int DT> struct AtWave {
             const float mf = -m[t] * f[t];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                float e = at_exp2(fmaf(y[t][i], f[t], mf));
-                if (!whole && y[t][i] == -INFINITY) e = 0.0f;
+                const float e = at_exp2(fmaf(y[t][i], f[t], mf));
                 l[t] += e;
                 lv[t] = fmaf(e, bv[i], lv[t]);
                 const float w = e * sv[i];
@@ -434,12 +463,30 @@ template <int D, int NCT, int DT> struct AtWave {
         }
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            const f16x8 a = at_codes(x.v[b]);
+            const f16x8 a = value(b);
 #pragma unroll
             for (int t = 0; t < NCT; ++t)
-#pragma unroll
-                for (int z = 0; z < PIECES; ++z) o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][z], o[t][b], 0, 0, 0);
+                if constexpr (PIECES == 1) {
+                    o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][0], o[t][b], 0, 0, 0);
+                } else {
+                    // added up outside the matrix unit: its sums of the whole row drift by a few 2^-18 (measured 3e-6 of the answer at
+                    // 1000 tokens; so 7e-7, the plain fp32 form's error)
+                    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+                    const f32x4 part = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][1], zero, 0, 0, 0);
+                    o[t][b] += __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][0], part, 0, 0, 0);
+                }
         }
+    }
+
+    // One wave for itself: 32 tokens that it has loaded.  `mem`: this wave's own.
+    __device__ __forceinline__ void step_alone(const Raw &x, float2 *mem, const AtMagic &magic, uint32_t t0, bool whole, bool there)
+    {
+        mem[threadIdx.x % kWave] = centred(x.grid);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        step([&](int j, int k) { return at_codes(x.k[j][k], magic); }, [&](int b) { return at_codes(x.v[b], magic); }, mem, t0, whole, there);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
 
     // The sums of all lanes of a column; o becomes the numerator, m the maximum in log2.
@@ -452,7 +499,7 @@ template <int D, int NCT, int DT> struct AtWave {
             l[t] += kv_xor_f32(l[t], 32);
             lv[t] += kv_xor_f32(lv[t], 16);
             lv[t] += kv_xor_f32(lv[t], 32);
-            m[t] = l[t] == 0.0f ? -3.402823466e38f : m[t] * f[t];
+            m[t] = l[t] == 0.0f ? -3.402823466e38f : m[t] * f[t];   // (a column that saw nothing: below any other)
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -461,6 +508,13 @@ template <int D, int NCT, int DT> struct AtWave {
     }
 };
 
+#ifndef QP_W1
+#define QP_W1 2
+#endif
+#ifndef QP_W2
+#define QP_W2 2
+#endif
+template <int D, int NCT, int DT> constexpr int kAtResident = D > 128 ? 1 : NCT == 1 ? QP_W1 : DT == QP_F32 ? 1 : QP_W2;
 __device__ __forceinline__ uint32_t at_bf16(float f)
 {
     const uint32_t u = __float_as_uint(f);
@@ -468,14 +522,25 @@ __device__ __forceinline__ uint32_t at_bf16(float f)
 }
 
 template <int D, int NCT, int DT>
-__global__ __launch_bounds__(kAtThreads) void k_kv_attention(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
+__global__ __launch_bounds__(kAtThreads, (kAtResident<D, NCT, DT>)) void k_kv_attention(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
 {
     using Wave = AtWave<D, NCT, DT>;
     constexpr int NB = Wave::NB;
-    // two waves' numerators and (m, sum), when the four waves of an item with split tokens are joined
-    __shared__ __align__(16) float nums[2][16 * NCT][D + 4];
-    __shared__ float2 sums[2][16 * NCT];
-    __shared__ __align__(16) float2 grids[kAtWaves][64];
+    // either: two waves' numerators and (m, sum), when the four waves of an item with split tokens are joined, and their grids;
+    // or: two steps' fragments, keys' and values', and grids, which the four waves of an item with split columns share
+    constexpr int kFrags = 2 * Wave::KS + NB;
+    struct Alone {
+        float nums[2][16 * NCT][D + 4];
+        float2 sums[2][16 * NCT];
+        float2 grids[kAtWaves][64];
+    };
+    struct Shared {
+        f16x8 frags[2][kFrags][kWave];
+        float2 grids[2][64];
+    };
+    __shared__ __align__(16) unsigned char mem[sizeof(Alone) > sizeof(Shared) ? sizeof(Alone) : sizeof(Shared)];
+    Alone &alone = *reinterpret_cast<Alone *>(mem);
+    Shared &shared = *reinterpret_cast<Shared *>(mem);
     AtPiece me;
     if (!at_find<NCT>(c, a, w, blockIdx.x, me)) return;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u;
@@ -505,6 +570,7 @@ __global__ __launch_bounds__(kAtThreads) void k_kv_attention(KvLayer c, KvView q
     const uint32_t tile_a = first + (uint32_t)((uint64_t)tiles * me.s / pieces), tile_b = first + (uint32_t)((uint64_t)tiles * (me.s + 1u) / pieces);
     uint32_t a0 = tile_a * kAtTile, a1 = min(tile_b * kAtTile, t_hi);        // this piece's tokens
     const uint32_t col1 = min(item1, col0 + 16u * NCT);
+    const uint32_t b0 = a0, b1 = a1;
     if (!split_tokens && col0 < col1) {       // ... and what this wave's columns see of them
         uint32_t w_lo, w_hi;
         range(col0, col1, w_lo, w_hi);
@@ -525,25 +591,85 @@ __global__ __launch_bounds__(kAtThreads) void k_kv_attention(KvLayer c, KvView q
         sees_lo = max(sees_lo, (int32_t)__shfl_xor((uint32_t)sees_lo, d, kWave));
         sees_hi = min(sees_hi, (int32_t)__shfl_xor((uint32_t)sees_hi, d, kWave));
     }
-    const uint32_t stride = split_tokens ? kAtTile : kAtStep;
-    uint32_t t0 = a0 + (split_tokens ? wave * kAtStep : 0u);
-    const auto page_at = [&](uint32_t t) { return kv_page(c, r, t >> c.page_shift); };
-    const auto slab_of = [&](int32_t page) { return kv_slab(c, page < 0 ? 0 : page, head); };
-    typename Wave::Raw cur, nxt;
-    int32_t page = -1, page_next = -1;
-    if (t0 < a1) {
-        page = __builtin_amdgcn_readfirstlane(page_at(t0));
-        page_next = t0 + stride < a1 ? page_at(t0 + stride) : -1;
-        x.load(cur, slab_of(page), t0, c.page_shift, row.length, page >= 0);
-    }
-    for (; t0 < a1; t0 += stride) {
-        const int32_t pn = __builtin_amdgcn_readfirstlane(page_next);
-        page_next = t0 + 2u * stride < a1 ? page_at(t0 + 2u * stride) : -1;
-        if (t0 + stride < a1) x.load(nxt, slab_of(pn), t0 + stride, c.page_shift, row.length, pn >= 0);
-        const bool whole = page >= 0 && (int32_t)t0 >= sees_lo && (int32_t)(t0 + kAtStep) <= sees_hi;
-        x.step(cur, grids[wave], t0, whole, page >= 0);
-        cur = nxt;
-        page = pn;
+    const auto slab_at = [&](uint32_t t, bool &there) {
+        const int32_t page = __builtin_amdgcn_readfirstlane(kv_page(c, r, t >> c.page_shift));
+        there = page >= 0;
+        return kv_slab(c, there ? page : 0, head);
+    };
+    const AtMagic magic;
+    if (split_tokens) {
+        uint32_t t0 = a0 + wave * kAtStep;
+        typename Wave::Raw cur, nxt;
+        bool there = false, there_next = false;
+        if (t0 < a1) {
+            const unsigned char *slab = slab_at(t0, there);
+            x.load(cur, slab, t0, c.page_shift, row.length, there);
+        }
+        for (; t0 < a1; t0 += kAtTile) {
+            if (t0 + kAtTile < a1) {
+                const unsigned char *slab = slab_at(t0 + kAtTile, there_next);
+                x.load(nxt, slab, t0 + kAtTile, c.page_shift, row.length, there_next);
+            }
+            const bool whole = there && (int32_t)t0 >= sees_lo && (int32_t)(t0 + kAtStep) <= sees_hi;
+            x.step_alone(cur, alone.grids[wave], magic, t0, whole, there);
+            cur = nxt;
+            there = there_next;
+        }
+    } else {
+        // every wave takes a quarter of a step's words apart for all of them; while a step runs the next one's fragments go to the
+        // other half of LDS and the words of the one after it are on their way
+        constexpr int kMine = (kFrags + kAtWaves - 1) / kAtWaves;
+        uint32_t words[kMine];
+        float2 grid{0.0f, 0.0f};
+        bool there = false, there_next = false, there_far = false;
+        const auto fetch = [&](uint32_t t, bool &is) {
+            const unsigned char *slab = slab_at(t, is);
+            const uint32_t pt = 1u << c.page_shift, in = t & (pt - 1u);
+            const uint32_t *kc = reinterpret_cast<const uint32_t *>(slab), *vc = kc + (size_t)pt * (D / kKvCodes);
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const uint32_t fr = kAtWaves * i + wave;      // fragment: keys (j, k), then values (b)
+                if (fr < 2u * Wave::KS)
+                    words[i] = kc[(size_t)(in + 8u * (n / 4u) + 4u * (fr / Wave::KS) + n % 4u) * (D / kKvCodes) + g * Wave::KS + fr % Wave::KS];
+                else if (fr < (uint32_t)kFrags)
+                    words[i] = vc[(size_t)(in / 8u + g) * D + n * NB + (fr - 2u * Wave::KS)];
+            }
+            if (wave == 0u) {
+                const float2 *grids = reinterpret_cast<const float2 *>(vc + (size_t)pt * (D / kKvCodes));
+                grid = grids[(lane < 32u ? 0u : pt) + in + lane % 32u];
+                if (!is || (int32_t)(t + lane % 32u) >= row.length) grid = float2{0.0f, 0.0f};
+            }
+        };
+        const auto put = [&](uint32_t half) {
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const uint32_t fr = kAtWaves * i + wave;
+                if (fr < (uint32_t)kFrags) shared.frags[half][fr][lane] = at_codes(words[i], magic);
+            }
+            if (wave == 0u) shared.grids[half][lane] = Wave::centred(grid);
+        };
+        uint32_t t = b0, half = 0u;
+        if (t < b1) {
+            fetch(t, there);
+            put(0u);
+            if (t + kAtStep < b1) fetch(t + kAtStep, there_next);
+        }
+        __syncthreads();
+        for (; t < b1; t += kAtStep) {
+            if (t + kAtStep < b1) {
+                put(half ^ 1u);
+                if (t + 2u * kAtStep < b1) fetch(t + 2u * kAtStep, there_far);
+            }
+            if (t >= a0 && t < a1) {
+                const bool whole = there && (int32_t)t >= sees_lo && (int32_t)(t + kAtStep) <= sees_hi;
+                x.step([&](int j, int k) { return shared.frags[half][j * Wave::KS + k][lane]; },
+                       [&](int b) { return shared.frags[half][2 * Wave::KS + b][lane]; }, shared.grids[half], t, whole, there);
+            }
+            __syncthreads();
+            half ^= 1u;
+            there = there_next;
+            there_next = there_far;
+        }
     }
     x.finish();
     if (split_tokens) {                       // waves 2, 3 into 0, 1, then 1 into 0
@@ -552,20 +678,20 @@ __global__ __launch_bounds__(kAtThreads) void k_kv_attention(KvLayer c, KvView q
             if (wave >= half && wave < 2u * half) {
 #pragma unroll
                 for (int t = 0; t < NCT; ++t) {
-                    float *dst = &nums[wave - half][16 * t + n][4u * NB * g];
+                    float *dst = &alone.nums[wave - half][16 * t + n][4u * NB * g];
 #pragma unroll
                     for (int r4 = 0; r4 < 4; ++r4)
 #pragma unroll
                         for (int b = 0; b < NB; ++b) dst[r4 * NB + b] = x.o[t][b][r4];
-                    if (g == 0u) sums[wave - half][16 * t + n] = float2{x.m[t], x.l[t]};
+                    if (g == 0u) alone.sums[wave - half][16 * t + n] = float2{x.m[t], x.l[t]};
                 }
             }
             __syncthreads();
             if (wave < half) {
 #pragma unroll
                 for (int t = 0; t < NCT; ++t) {
-                    const float *src = &nums[wave][16 * t + n][4u * NB * g];
-                    const float2 other = sums[wave][16 * t + n];
+                    const float *src = &alone.nums[wave][16 * t + n][4u * NB * g];
+                    const float2 other = alone.sums[wave][16 * t + n];
                     const float top = fmaxf(x.m[t], other.x), ea = at_exp2(x.m[t] - top), eb = at_exp2(other.x - top);
                     x.m[t] = top;
                     x.l[t] = fmaf(x.l[t], ea, other.y * eb);

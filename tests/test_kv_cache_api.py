@@ -125,7 +125,7 @@ def test_books_that_are_refused(qp):
         assert call(qp, make(qp, books=FAKE + 2)) == qp.QP_EINVAL
     for call in BOOKS + [compact]:
         assert call(qp, make(qp, pool=None)) == qp.QP_EINVAL
-        assert call(qp, make(qp, pool=FAKE + 4)) == qp.QP_EINVAL
+        assert call(qp, make(qp, pool=FAKE + 2)) == qp.QP_EINVAL
     assert qp.lib().qp_kv_pool_init(0, FAKE, 1 << 40, None) == qp.QP_EINVAL
     assert qp.lib().qp_kv_pool_init((1 << 24) + 1, FAKE, 1 << 40, None) == qp.QP_EINVAL
     assert qp.lib().qp_kv_pool_init(4, None, 1 << 40, None) == qp.QP_EINVAL
