@@ -206,10 +206,8 @@ size_t qp_kv_attention_workspace_bytes(const qp_kv_cache_t *cache, const qp_kv_r
     if (q_heads == 0u || q_heads % cache->kv_heads || q_heads / cache->kv_heads > 1024u) return 0;
     if (tokens >= (1ull << 31) || tokens * q_heads >= (1ull << 31)) return 0;
     const KvLayer c = layer_of(cache, rows, 0, nullptr, tokens);
-    size_t narrow, wide;
-    (void)at_work<1>(nullptr, c, cache->head_dim, q_heads / cache->kv_heads, narrow);
-    (void)at_work<2>(nullptr, c, cache->head_dim, q_heads / cache->kv_heads, wide);
-    return at_narrow(q_heads / cache->kv_heads, rows->rows, tokens) ? narrow : wide;
+    size_t few;
+    return at_bytes(c, cache->head_dim, q_heads / cache->kv_heads, few);
 }
 
 qp_status qp_kv_attention(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, uint32_t layer, const int32_t *token_begin_dev,

@@ -24,12 +24,16 @@
 // The maximum is lazy: a column's m moves only when a lane sees a score more than 8 (in log2) above it, so the loop has no exchange
 // between lanes; what is rare (the maximum moves, N moves) is one branch of the whole wave.
 //
-// Who does what.  A block (four waves) takes one item: 64 NCT columns of one row and key head (each wave a quarter of the columns,
-// all tokens), or, if it has at most 16 NCT columns, all waves the same columns and every fourth 32 tokens each, joined
-// through LDS at the end.  Rows' lengths are known to the device only: every block adds up the whole call's work from them
-// (a few hundred lengths: one load a lane) and finds which item, and which of S equal pieces of its tokens, is its own, so that
-// about kvTarget pieces come out whatever the lengths.  Pieces leave (m, sum p, numerators) in the workspace, and a second
-// kernel joins them in order.
+// Who does what.  An item is some columns of one row and key head, a block (four waves) takes an item or a piece of its tokens:
+//   few    16 columns; every wave all of them and every fourth 32 tokens, joined through LDS at the end.  What a single token of a
+//          row, or a few of them, need: bound by HBM, (head_dim + 16) bytes for each token and key head.
+//   many   128 columns, 32 a wave; all waves the same tokens, whose words each wave takes apart a quarter of and shares through
+//          LDS.  Prompts: bound by vector instructions (about 7 for each score beside the matrix units' work).
+// A call whose rows bring 16 columns or fewer on average goes to `few` alone; else rows are cut into 128 columns for `many`, and
+// a rest of 16 or fewer goes to `few` (single tokens in a batch with prompts).  Rows' lengths are known to the device only: every
+// block adds up the whole call's work from them (a few hundred lengths: one load a lane) and finds which item, and which of S
+// equal pieces of its tokens, is its own, so that about as many pieces come out as the chip runs at a time, whatever the
+// lengths.  Pieces leave (m, sum p, numerators) in the workspace, and a last kernel joins them in order.
 #pragma once
 
 #include "qp_kv.hpp"
@@ -39,82 +43,100 @@ namespace qp {
 constexpr int kAtThreads = 256, kAtWaves = 4;
 constexpr uint32_t kAtStep = 32;                 // tokens of a wave's step
 constexpr uint32_t kAtTile = kAtStep * kAtWaves; // tokens that work is counted in
-#ifndef QP_KV_TARGET
-#define QP_KV_TARGET 1024
+constexpr uint32_t kAtUnit = 16;                 // columns that partial results are counted in
+template <bool MANY> constexpr uint32_t kAtCols = MANY ? 128u : kAtUnit;     // columns of an item
+// pieces that a call is cut into, and tiles that one has at least (joining costs a kernel and a pass over the pieces, more than
+// it takes to go through these)
+#ifndef QP_KV_FEW
+#define QP_KV_FEW 512
 #endif
-// pieces that a call is cut into: what the chip runs at the same time
-template <int NCT> constexpr uint32_t kAtTarget = NCT == 1 ? QP_KV_TARGET : QP_KV_TARGET / 2;
-// tiles that a piece has at least: joining costs a kernel and a pass over the pieces, more than it takes to go through these
+#ifndef QP_KV_MANY
+#define QP_KV_MANY 320
+#endif
 #ifndef QP_KV_LEAST
 #define QP_KV_LEAST 4
 #endif
+template <bool MANY> constexpr uint32_t kAtTarget = MANY ? QP_KV_MANY : QP_KV_FEW;
 constexpr uint32_t kAtLeast = QP_KV_LEAST;
 constexpr float kAtHeadroom = 8.0f;              // log2 that a score may lie above its column's m
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-// The workspace: [0] columns that were split; a record for each; (m, sum) and numerators of the pieces, in units of 16 NCT columns.
+// A part of the workspace, for one kind of items: [0] columns that were split; a record for each; (m, sum) and numerators of the
+// pieces, in units of 16 columns.
 struct AtWork {
     uint32_t *header;
     u32x4 *cols;
     float2 *sums;
     float *nums;
     uint32_t most_cols, most_units;
+    uint32_t wide;                               // rows are cut into 128 columns first
 };
 constexpr size_t kAtHeader = 256;
-inline uint64_t at_items(uint32_t nct, const KvLayer &c, uint32_t group)      // a row has one for each 64 nct columns begun
+// Columns that a wave of `few` shall not take one by one: see above.
+inline bool at_wide(uint32_t group, uint32_t rows, uint64_t tokens) { return tokens * group > (uint64_t)kAtUnit * rows; }
+template <bool MANY> uint64_t at_items(const KvLayer &c, uint32_t group)     // at most; a row has one for each kAtCols begun
 {
     const uint64_t rows = c.rows < c.tokens ? c.rows : c.tokens;
-    return c.kv_heads * ((uint64_t)c.tokens * group / (64u * nct) + rows);
+    if (!MANY && at_wide(group, c.rows, c.tokens)) return c.kv_heads * rows;
+    return c.kv_heads * ((uint64_t)c.tokens * group / kAtCols<MANY> + rows);
 }
 // An item of n tiles is cut up if n exceeds a piece's share, and then into less than n / share + 1 <= 2 n / share pieces: twice
 // the target at most for all of them, in target items at most.
-template <int NCT> AtWork at_work(void *ws, const KvLayer &c, uint32_t dim, uint32_t group, size_t &bytes)
+template <bool MANY> AtWork at_work(char *ws, const KvLayer &c, uint32_t dim, uint32_t group, size_t &bytes)
 {
-    const uint64_t tiles = (((uint64_t)c.pages_per_row << c.page_shift) + kAtTile - 1u) / kAtTile, items = at_items(NCT, c, group);
-    const uint64_t columns = (uint64_t)c.tokens * c.kv_heads * group, target = kAtTarget<NCT>;
-    // a piece's share is at least kAtLeast tiles, a quarter of them where the waves split columns
-    const uint64_t least = (uint64_t)c.tokens * group > 16u * NCT ? (kAtLeast + 3u) / 4u : kAtLeast;
-    uint64_t pieces = tiles <= least ? 0u : 2u * target, cols = tiles <= least ? 0u : target * 64u * NCT;
-    if (items < 2u * target && items * tiles < pieces) pieces = items * tiles;   // (one tile each at the least)
+    const uint64_t tiles = (((uint64_t)c.pages_per_row << c.page_shift) + kAtTile - 1u) / kAtTile, items = at_items<MANY>(c, group);
+    const uint64_t columns = (uint64_t)c.tokens * c.kv_heads * group, target = kAtTarget<MANY>;
+    uint64_t pieces = tiles <= kAtLeast ? 0u : 2u * target, cols = tiles <= kAtLeast ? 0u : target * kAtCols<MANY>;
+    if (items < 2u * target && items * tiles < pieces) pieces = items * tiles;
     if (columns < cols) cols = columns;
     AtWork w{};
-    w.most_units = (uint32_t)(pieces * ((uint64_t)c.tokens * group > 16u * NCT ? 4u : 1u));
+    w.wide = at_wide(group, c.rows, c.tokens) ? 1u : 0u;
+    w.most_units = (uint32_t)(pieces * (kAtCols<MANY> / kAtUnit));
     w.most_cols = (uint32_t)cols;
-    const size_t sums = kAtHeader + (size_t)cols * sizeof(u32x4), nums = sums + (size_t)w.most_units * 16u * NCT * sizeof(float2);
-    bytes = nums + (size_t)w.most_units * 16u * NCT * dim * sizeof(float);
-    if (char *p = static_cast<char *>(ws)) {
-        w.header = reinterpret_cast<uint32_t *>(p);
-        w.cols = reinterpret_cast<u32x4 *>(p + kAtHeader);
-        w.sums = reinterpret_cast<float2 *>(p + sums);
-        w.nums = reinterpret_cast<float *>(p + nums);
+    const size_t sums = kAtHeader + (size_t)cols * sizeof(u32x4), nums = sums + (size_t)w.most_units * kAtUnit * sizeof(float2);
+    bytes = nums + (size_t)w.most_units * kAtUnit * dim * sizeof(float);
+    if (ws) {
+        w.header = reinterpret_cast<uint32_t *>(ws);
+        w.cols = reinterpret_cast<u32x4 *>(ws + kAtHeader);
+        w.sums = reinterpret_cast<float2 *>(ws + sums);
+        w.nums = reinterpret_cast<float *>(ws + nums);
     }
     return w;
 }
+// The whole workspace of a call.
+inline size_t at_bytes(const KvLayer &c, uint32_t dim, uint32_t group, size_t &few)
+{
+    size_t many = 0;
+    (void)at_work<false>(nullptr, c, dim, group, few);
+    if (at_wide(group, c.rows, c.tokens)) (void)at_work<true>(nullptr, c, dim, group, many);
+    few = (few + 255u) / 256u * 256u;
+    return few + many;
+}
 
 // ---- which piece of which item a block has ---------------------------------------------------------------------------------
-struct AtRow {               // a row's items: n4 with the columns split among the waves, n1 (0 or 1) with the tokens split
-    uint32_t n4, n1, tiles, cols;
+struct AtRow {
+    uint32_t items, first, cols, tiles;          // items from column `first` on; `cols`: where the last one ends
 };
-template <int NCT> __device__ __forceinline__ AtRow at_row(const KvLayer &c, const KvAttn &a, uint32_t r)
+template <bool MANY> __device__ __forceinline__ AtRow at_row(const KvLayer &c, const KvAttn &a, bool wide, uint32_t r)
 {
     const KvRow row = kv_row(c, r);
     AtRow o;
-    o.cols = (uint32_t)row.count * a.group;
-    const uint32_t full = o.cols / (64u * NCT), rest = o.cols % (64u * NCT);
-    o.n1 = rest != 0u && rest <= 16u * NCT ? 1u : 0u;
-    o.n4 = full + (rest > 16u * NCT ? 1u : 0u);
+    const uint32_t cols = (uint32_t)row.count * a.group, rest = cols % kAtCols<true>;
+    const bool small = rest <= kAtUnit;          // the rest is for `few`
+    o.first = !MANY && wide ? (small ? cols - rest : cols) : 0u;
+    o.cols = MANY && small ? cols - rest : cols;
+    o.items = (o.cols - o.first + kAtCols<MANY> - 1u) / kAtCols<MANY>;
     const int64_t from = a.window ? (int64_t)row.length - row.count - a.window + 1 : 0;
     const uint32_t lo = from > 0 ? (uint32_t)from / kAtTile : 0u, hi = ((uint32_t)row.length + kAtTile - 1u) / kAtTile;
     o.tiles = hi > lo ? hi - lo : 1u;
     return o;
 }
 struct AtPiece {
-    uint32_t row, head, ct, s, pieces;       // pieces: at most so many of the item's tokens
-    uint32_t per;                            // tiles that a piece should have
-    uint32_t unit, unit_step;                // where the item's partial results go (piece s at unit + s unit_step)
-    uint32_t col;                            // ... and its columns' records
+    uint32_t row, head, col0, col1, s, pieces;   // columns; pieces: at most so many of the item's tokens
+    uint32_t per;                                // tiles that a piece should have
+    uint32_t unit, rec;                          // where the item's partial results and its columns' records go
 };
 // Inclusive prefix sums of three numbers over the block; `part` holds each wave's totals.
 __device__ __forceinline__ void at_scan(uint32_t (&x)[3], uint32_t (*part)[3], uint32_t (&total)[3])
@@ -149,69 +171,54 @@ __device__ __forceinline__ uint64_t at_wave_sum(uint64_t v)
 }
 
 // False: the call has fewer pieces than blocks.
-template <int NCT>
-__device__ __forceinline__ bool at_find(const KvLayer &c, const KvAttn &a, const AtWork &w, uint32_t block, AtPiece &mine)
+template <bool MANY> __device__ __forceinline__ bool at_find(const KvLayer &c, const KvAttn &a, const AtWork &w, uint32_t block, AtPiece &mine)
 {
+    constexpr uint32_t kUnits = kAtCols<MANY> / kAtUnit;
     __shared__ uint32_t part[kAtWaves][3];
     __shared__ uint64_t work[kAtWaves];
     __shared__ AtPiece found;
     __shared__ uint32_t have, split;
     const uint32_t tid = threadIdx.x;
-    const AtRow none{0u, 0u, 1u, 0u};
-    const AtRow mine0 = tid < c.rows ? at_row<NCT>(c, a, tid) : none;      // (most calls have no more rows than that)
-    uint64_t cost = (uint64_t)mine0.tiles * (mine0.n4 * 4u + mine0.n1);
+    const AtRow none{0u, 0u, 0u, 1u};
+    const AtRow mine0 = tid < c.rows ? at_row<MANY>(c, a, w.wide, tid) : none;      // (most calls have no more rows than that)
+    uint64_t cost = (uint64_t)mine0.tiles * mine0.items;
     for (uint32_t r = tid + kAtThreads; r < c.rows; r += kAtThreads) {
-        const AtRow o = at_row<NCT>(c, a, r);
-        cost += (uint64_t)o.tiles * (o.n4 * 4u + o.n1);
+        const AtRow o = at_row<MANY>(c, a, w.wide, r);
+        cost += (uint64_t)o.tiles * o.items;
     }
     cost = at_wave_sum(cost);
     if (tid % kWave == 0u) work[tid / kWave] = cost;
     if (tid == 0u) have = split = 0u;
     __syncthreads();
     const uint64_t all = (work[0] + work[1] + work[2] + work[3]) * c.kv_heads;
-    const uint64_t share = max((all + kAtTarget<NCT> - 1u) / kAtTarget<NCT>, (uint64_t)kAtLeast);
-    const uint32_t per1 = (uint32_t)min(share, (uint64_t)0x7fffffffu), per4 = (uint32_t)min((share + 3u) / 4u, (uint64_t)0x7fffffffu);
+    const uint32_t per = (uint32_t)min(max((all + kAtTarget<MANY> - 1u) / kAtTarget<MANY>, (uint64_t)kAtLeast), (uint64_t)0x7fffffffu);
     uint32_t before[3] = {0u, 0u, 0u};                   // blocks, units, columns of the rows so far
     for (uint32_t r0 = 0; r0 < c.rows; r0 += kAtThreads) {
         const uint32_t r = r0 + tid;
-        const AtRow o = r0 == 0u ? mine0 : r < c.rows ? at_row<NCT>(c, a, r) : none;
-        const uint32_t s4 = (o.tiles + per4 - 1u) / per4, s1 = (o.tiles + per1 - 1u) / per1;
-        const uint32_t last = o.n1 ? o.cols - o.n4 * 64u * NCT : 0u;          // columns of the item with split tokens
-        const uint32_t b4 = c.kv_heads * o.n4 * s4, b1 = c.kv_heads * o.n1 * s1;
-        const uint32_t u4 = s4 > 1u ? 4u * b4 : 0u, u1 = s1 > 1u ? b1 : 0u;
-        const uint32_t k4 = s4 > 1u ? c.kv_heads * (o.cols - last) : 0u, k1 = s1 > 1u ? c.kv_heads * last : 0u;
-        uint32_t x[3] = {b4 + b1, u4 + u1, k4 + k1}, total[3];
+        const AtRow o = r0 == 0u ? mine0 : r < c.rows ? at_row<MANY>(c, a, w.wide, r) : none;
+        const uint32_t pieces = (o.tiles + per - 1u) / per, blocks = c.kv_heads * o.items * pieces;
+        const uint32_t units = pieces > 1u ? blocks * kUnits : 0u, cols = pieces > 1u ? c.kv_heads * (o.cols - o.first) : 0u;
+        uint32_t x[3] = {blocks, units, cols}, total[3];
         at_scan(x, part, total);
         const uint32_t eb = before[0] + x[0], eu = before[1] + x[1], ek = before[2] + x[2];      // ends
-        const uint32_t pb = eb - (b4 + b1), pu = eu - (u4 + u1), pk = ek - (k4 + k1);
+        const uint32_t pb = eb - blocks, pu = eu - units, pk = ek - cols;
         // (always so where the rows' tokens do not overlap: what the host sized the grid and the workspace for)
         const bool fits = pb <= gridDim.x && eb <= gridDim.x && pu <= w.most_units && eu <= w.most_units && pk <= w.most_cols && ek <= w.most_cols;
-        if (fits && k4 + k1 != 0u) atomicMax(&split, ek);
+        if (fits && cols != 0u) atomicMax(&split, ek);
         if (fits && block >= pb && block < eb) {
-            uint32_t i = block - pb;
+            uint32_t i = block - pb;                     // heads side by side: an XCD per head, whose tokens its L2 then holds
             AtPiece f;
             f.row = r;
-            if (i < b4) {        // the last columns, which see the most tokens, first; heads side by side: an XCD per head
-                f.head = i % c.kv_heads;
-                i /= c.kv_heads;
-                f.s = i % s4;
-                f.ct = o.n4 - 1u - i / s4;
-                f.pieces = s4;
-                f.per = per4;
-                f.unit = pu + (f.ct * c.kv_heads + f.head) * s4 * 4u;
-                f.unit_step = 4u;
-                f.col = pk + f.ct * 64u * NCT * c.kv_heads + f.head * min(64u * NCT, o.cols - f.ct * 64u * NCT);
-            } else {
-                i -= b4;
-                f.head = i % c.kv_heads;
-                f.s = i / c.kv_heads;
-                f.ct = o.n4;
-                f.pieces = s1;
-                f.per = per1;
-                f.unit = pu + u4 + f.head * s1;
-                f.unit_step = 1u;
-                f.col = pk + k4 + f.head * last;
-            }
+            f.head = i % c.kv_heads;
+            i /= c.kv_heads;
+            f.s = i % pieces;
+            const uint32_t item = o.items - 1u - i / pieces;       // the last columns, which see the most tokens, first
+            f.col0 = o.first + item * kAtCols<MANY>;
+            f.col1 = min(f.col0 + kAtCols<MANY>, o.cols);
+            f.pieces = pieces;
+            f.per = per;
+            f.unit = pu + (item * c.kv_heads + f.head) * pieces * kUnits;
+            f.rec = pk + (f.col0 - o.first) * c.kv_heads + f.head * (f.col1 - f.col0);
             found = f;
             have = 1u;
         }
@@ -508,203 +515,76 @@ template <int D, int NCT, int DT> struct AtWave {
     }
 };
 
-#ifndef QP_W1
-#define QP_W1 2
-#endif
-#ifndef QP_W2
-#define QP_W2 2
-#endif
-template <int D, int NCT, int DT> constexpr int kAtResident = D > 128 ? 1 : NCT == 1 ? QP_W1 : DT == QP_F32 ? 1 : QP_W2;
 __device__ __forceinline__ uint32_t at_bf16(float f)
 {
     const uint32_t u = __float_as_uint(f);
     return (u & 0x7fffffffu) > 0x7f800000u ? (u >> 16) | 0x40u : (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
 }
 
-template <int D, int NCT, int DT>
-__global__ __launch_bounds__(kAtThreads, (kAtResident<D, NCT, DT>)) void k_kv_attention(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
+// What a block of either kind knows of its piece.
+struct AtBlock {
+    KvRow row;
+    AtPiece p;
+    uint32_t pieces;             // of the item, as many as it has tiles for
+    uint32_t t0, t1;             // the piece's tokens; t0 a multiple of kAtTile
+};
+// the tokens that any of the row's columns [from, to) sees
+__device__ __forceinline__ void at_range(const KvRow &row, const KvAttn &a, uint32_t from, uint32_t to, uint32_t &lo, uint32_t &hi)
 {
-    using Wave = AtWave<D, NCT, DT>;
-    constexpr int NB = Wave::NB;
-    // either: two waves' numerators and (m, sum), when the four waves of an item with split tokens are joined, and their grids;
-    // or: two steps' fragments, keys' and values', and grids, which the four waves of an item with split columns share
-    constexpr int kFrags = 2 * Wave::KS + NB;
-    struct Alone {
-        float nums[2][16 * NCT][D + 4];
-        float2 sums[2][16 * NCT];
-        float2 grids[kAtWaves][64];
-    };
-    struct Shared {
-        f16x8 frags[2][kFrags][kWave];
-        float2 grids[2][64];
-    };
-    __shared__ __align__(16) unsigned char mem[sizeof(Alone) > sizeof(Shared) ? sizeof(Alone) : sizeof(Shared)];
-    Alone &alone = *reinterpret_cast<Alone *>(mem);
-    Shared &shared = *reinterpret_cast<Shared *>(mem);
-    AtPiece me;
-    if (!at_find<NCT>(c, a, w, blockIdx.x, me)) return;
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u;
-    const uint32_t r = __builtin_amdgcn_readfirstlane(me.row), head = __builtin_amdgcn_readfirstlane(me.head);
-    const KvRow row = kv_row(c, r);
-    const uint32_t cols = (uint32_t)row.count * a.group, item0 = me.ct * 64u * NCT, item1 = min(cols, item0 + 64u * NCT);
-    const bool split_tokens = me.unit_step == 1u;
-    const uint32_t col0 = item0 + (split_tokens ? 0u : wave * 16u * NCT);
-    // the tokens that any of the columns [from, to) sees
-    const auto range = [&](uint32_t from, uint32_t to, uint32_t &t_lo, uint32_t &t_hi) {
-        const int64_t first = (int64_t)row.length - row.count + from / a.group, last = (int64_t)row.length - row.count + (to - 1u) / a.group;
-        t_lo = a.window ? (uint32_t)max((int64_t)0, first - (int64_t)a.window + 1) : 0u;
-        t_hi = a.causal ? (uint32_t)max((int64_t)0, min(last + 1, (int64_t)row.length)) : (uint32_t)row.length;
-        if (t_lo > t_hi) t_lo = t_hi;
-    };
-    uint32_t t_lo, t_hi;
-    range(item0, item1, t_lo, t_hi);
-    const uint32_t first = t_lo / kAtTile, tiles = t_hi > t_lo ? (t_hi + kAtTile - 1u) / kAtTile - first : 0u;
-    const uint32_t pieces = max(1u, min(me.pieces, (tiles + me.per - 1u) / me.per));
-    if (me.pieces > 1u && me.s == 0u)         // the columns' records for the kernel that joins them
-        for (uint32_t k = threadIdx.x; k < item1 - item0; k += kAtThreads) {
-            const uint32_t col = item0 + k, unit = me.unit + (split_tokens ? 0u : k / (16u * NCT));
-            const uint32_t place = (uint32_t)(row.begin + (int32_t)(col / a.group)), h = head * a.group + col % a.group;
-            w.cols[me.col + k] = u32x4{unit * (16u * NCT) + k % (16u * NCT), pieces > 1u ? pieces : 0u, me.unit_step * (16u * NCT), place * (c.kv_heads * a.group) + h};
+    const int64_t start = (int64_t)row.length - row.count;
+    const int64_t first = start + from / a.group, last = start + (to - 1u) / a.group;
+    lo = a.window ? (uint32_t)max((int64_t)0, first - (int64_t)a.window + 1) : 0u;
+    hi = a.causal ? (uint32_t)max((int64_t)0, min(last + 1, (int64_t)row.length)) : (uint32_t)row.length;
+    if (lo > hi) lo = hi;
+}
+template <bool MANY> __device__ __forceinline__ bool at_begin(const KvLayer &c, const KvAttn &a, const AtWork &w, AtBlock &b)
+{
+    if (!at_find<MANY>(c, a, w, blockIdx.x, b.p)) return false;
+    AtPiece &p = b.p;
+    p.row = __builtin_amdgcn_readfirstlane(p.row);
+    p.head = __builtin_amdgcn_readfirstlane(p.head);
+    p.col0 = __builtin_amdgcn_readfirstlane(p.col0);
+    p.col1 = __builtin_amdgcn_readfirstlane(p.col1);
+    b.row = kv_row(c, p.row);
+    uint32_t lo, hi;
+    at_range(b.row, a, p.col0, p.col1, lo, hi);
+    const uint32_t first = lo / kAtTile, tiles = hi > lo ? (hi + kAtTile - 1u) / kAtTile - first : 0u;
+    b.pieces = max(1u, min(p.pieces, (tiles + p.per - 1u) / p.per));
+    if (p.pieces > 1u && p.s == 0u)           // the columns' records for the kernel that joins them
+        for (uint32_t k = threadIdx.x; k < p.col1 - p.col0; k += kAtThreads) {
+            const uint32_t col = p.col0 + k, place = (uint32_t)b.row.begin + col / a.group, h = p.head * a.group + col % a.group;
+            w.cols[p.rec + k] = u32x4{p.unit * kAtUnit + k, b.pieces > 1u ? b.pieces : 0u, kAtCols<MANY>, place * (c.kv_heads * a.group) + h};
         }
-    if (me.s >= pieces) return;
-    const uint32_t tile_a = first + (uint32_t)((uint64_t)tiles * me.s / pieces), tile_b = first + (uint32_t)((uint64_t)tiles * (me.s + 1u) / pieces);
-    uint32_t a0 = tile_a * kAtTile, a1 = min(tile_b * kAtTile, t_hi);        // this piece's tokens
-    const uint32_t col1 = min(item1, col0 + 16u * NCT);
-    const uint32_t b0 = a0, b1 = a1;
-    if (!split_tokens && col0 < col1) {       // ... and what this wave's columns see of them
-        uint32_t w_lo, w_hi;
-        range(col0, col1, w_lo, w_hi);
-        a0 = max(a0, w_lo / kAtStep * kAtStep);
-        a1 = min(a1, w_hi);
-    }
-    if (col0 >= col1) a1 = a0;
-    Wave x;
-    x.load_query(c, qv, a, row, head, col0, col1);
-    int32_t sees_lo = 0, sees_hi = 0x7fffffff;                               // what all of the wave's columns see
+    if (p.s >= b.pieces) return false;
+    b.t0 = (first + (uint32_t)((uint64_t)tiles * p.s / b.pieces)) * kAtTile;
+    b.t1 = min((first + (uint32_t)((uint64_t)tiles * (p.s + 1u) / b.pieces)) * kAtTile, hi);
+    return true;
+}
+// The tokens that all of a wave's columns see.
+template <typename Wave, int NCT> __device__ __forceinline__ void at_sees(const Wave &x, int32_t &lo, int32_t &hi)
+{
+    lo = 0;
+    hi = 0x7fffffff;
 #pragma unroll
     for (int t = 0; t < NCT; ++t) {
-        sees_lo = max(sees_lo, x.lo[t]);
-        sees_hi = min(sees_hi, x.hi[t]);
+        lo = max(lo, x.lo[t]);
+        hi = min(hi, x.hi[t]);
     }
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) {
-        sees_lo = max(sees_lo, (int32_t)__shfl_xor((uint32_t)sees_lo, d, kWave));
-        sees_hi = min(sees_hi, (int32_t)__shfl_xor((uint32_t)sees_hi, d, kWave));
+        lo = max(lo, (int32_t)__shfl_xor((uint32_t)lo, d, kWave));
+        hi = min(hi, (int32_t)__shfl_xor((uint32_t)hi, d, kWave));
     }
-    const auto slab_at = [&](uint32_t t, bool &there) {
-        const int32_t page = __builtin_amdgcn_readfirstlane(kv_page(c, r, t >> c.page_shift));
-        there = page >= 0;
-        return kv_slab(c, there ? page : 0, head);
-    };
-    const AtMagic magic;
-    if (split_tokens) {
-        uint32_t t0 = a0 + wave * kAtStep;
-        typename Wave::Raw cur, nxt;
-        bool there = false, there_next = false;
-        if (t0 < a1) {
-            const unsigned char *slab = slab_at(t0, there);
-            x.load(cur, slab, t0, c.page_shift, row.length, there);
-        }
-        for (; t0 < a1; t0 += kAtTile) {
-            if (t0 + kAtTile < a1) {
-                const unsigned char *slab = slab_at(t0 + kAtTile, there_next);
-                x.load(nxt, slab, t0 + kAtTile, c.page_shift, row.length, there_next);
-            }
-            const bool whole = there && (int32_t)t0 >= sees_lo && (int32_t)(t0 + kAtStep) <= sees_hi;
-            x.step_alone(cur, alone.grids[wave], magic, t0, whole, there);
-            cur = nxt;
-            there = there_next;
-        }
-    } else {
-        // every wave takes a quarter of a step's words apart for all of them; while a step runs the next one's fragments go to the
-        // other half of LDS and the words of the one after it are on their way
-        constexpr int kMine = (kFrags + kAtWaves - 1) / kAtWaves;
-        uint32_t words[kMine];
-        float2 grid{0.0f, 0.0f};
-        bool there = false, there_next = false, there_far = false;
-        const auto fetch = [&](uint32_t t, bool &is) {
-            const unsigned char *slab = slab_at(t, is);
-            const uint32_t pt = 1u << c.page_shift, in = t & (pt - 1u);
-            const uint32_t *kc = reinterpret_cast<const uint32_t *>(slab), *vc = kc + (size_t)pt * (D / kKvCodes);
-#pragma unroll
-            for (int i = 0; i < kMine; ++i) {
-                const uint32_t fr = kAtWaves * i + wave;      // fragment: keys (j, k), then values (b)
-                if (fr < 2u * Wave::KS)
-                    words[i] = kc[(size_t)(in + 8u * (n / 4u) + 4u * (fr / Wave::KS) + n % 4u) * (D / kKvCodes) + g * Wave::KS + fr % Wave::KS];
-                else if (fr < (uint32_t)kFrags)
-                    words[i] = vc[(size_t)(in / 8u + g) * D + n * NB + (fr - 2u * Wave::KS)];
-            }
-            if (wave == 0u) {
-                const float2 *grids = reinterpret_cast<const float2 *>(vc + (size_t)pt * (D / kKvCodes));
-                grid = grids[(lane < 32u ? 0u : pt) + in + lane % 32u];
-                if (!is || (int32_t)(t + lane % 32u) >= row.length) grid = float2{0.0f, 0.0f};
-            }
-        };
-        const auto put = [&](uint32_t half) {
-#pragma unroll
-            for (int i = 0; i < kMine; ++i) {
-                const uint32_t fr = kAtWaves * i + wave;
-                if (fr < (uint32_t)kFrags) shared.frags[half][fr][lane] = at_codes(words[i], magic);
-            }
-            if (wave == 0u) shared.grids[half][lane] = Wave::centred(grid);
-        };
-        uint32_t t = b0, half = 0u;
-        if (t < b1) {
-            fetch(t, there);
-            put(0u);
-            if (t + kAtStep < b1) fetch(t + kAtStep, there_next);
-        }
-        __syncthreads();
-        for (; t < b1; t += kAtStep) {
-            if (t + kAtStep < b1) {
-                put(half ^ 1u);
-                if (t + 2u * kAtStep < b1) fetch(t + 2u * kAtStep, there_far);
-            }
-            if (t >= a0 && t < a1) {
-                const bool whole = there && (int32_t)t >= sees_lo && (int32_t)(t + kAtStep) <= sees_hi;
-                x.step([&](int j, int k) { return shared.frags[half][j * Wave::KS + k][lane]; },
-                       [&](int b) { return shared.frags[half][2 * Wave::KS + b][lane]; }, shared.grids[half], t, whole, there);
-            }
-            __syncthreads();
-            half ^= 1u;
-            there = there_next;
-            there_next = there_far;
-        }
-    }
-    x.finish();
-    if (split_tokens) {                       // waves 2, 3 into 0, 1, then 1 into 0
-#pragma unroll
-        for (uint32_t half = 2; half >= 1; half /= 2) {
-            if (wave >= half && wave < 2u * half) {
-#pragma unroll
-                for (int t = 0; t < NCT; ++t) {
-                    float *dst = &alone.nums[wave - half][16 * t + n][4u * NB * g];
-#pragma unroll
-                    for (int r4 = 0; r4 < 4; ++r4)
-#pragma unroll
-                        for (int b = 0; b < NB; ++b) dst[r4 * NB + b] = x.o[t][b][r4];
-                    if (g == 0u) alone.sums[wave - half][16 * t + n] = float2{x.m[t], x.l[t]};
-                }
-            }
-            __syncthreads();
-            if (wave < half) {
-#pragma unroll
-                for (int t = 0; t < NCT; ++t) {
-                    const float *src = &alone.nums[wave][16 * t + n][4u * NB * g];
-                    const float2 other = alone.sums[wave][16 * t + n];
-                    const float top = fmaxf(x.m[t], other.x), ea = at_exp2(x.m[t] - top), eb = at_exp2(other.x - top);
-                    x.m[t] = top;
-                    x.l[t] = fmaf(x.l[t], ea, other.y * eb);
-#pragma unroll
-                    for (int r4 = 0; r4 < 4; ++r4)
-#pragma unroll
-                        for (int b = 0; b < NB; ++b) x.o[t][b][r4] = fmaf(x.o[t][b][r4], ea, src[r4 * NB + b] * eb);
-                }
-            }
-            __syncthreads();
-        }
-        if (wave != 0u) return;
-    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+}
+// A wave's columns [col0, col1): the answer, or the piece's part of it (`k0`: the first one's place in the item).
+template <int D, int NCT, int DT>
+__device__ __forceinline__ void at_store(const AtWave<D, NCT, DT> &x, const AtBlock &b, const KvAttn &a, const AtWork &w, const KvView &out, uint32_t item_cols,
+                                         uint32_t col0, uint32_t col1)
+{
+    constexpr int NB = AtWave<D, NCT, DT>::NB;
+    const uint32_t lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u;
 #pragma unroll
     for (int t = 0; t < NCT; ++t) {
         const uint32_t col = col0 + 16u * t + n;
@@ -713,43 +593,270 @@ __global__ __launch_bounds__(kAtThreads, (kAtResident<D, NCT, DT>)) void k_kv_at
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4)
 #pragma unroll
-            for (int b = 0; b < NB; ++b) v[r4 * NB + b] = x.o[t][b][r4];
-        if (pieces > 1u) {
-            const size_t at = (size_t)(me.unit + me.s * me.unit_step + (split_tokens ? 0u : wave)) * (16u * NCT) + 16u * t + n;
+            for (int i = 0; i < NB; ++i) v[r4 * NB + i] = x.o[t][i][r4];
+        if (b.pieces > 1u) {
+            const size_t at = (size_t)b.p.unit * kAtUnit + (size_t)b.p.s * item_cols + (col - b.p.col0);
             if (g == 0u) w.sums[at] = float2{x.m[t], x.l[t]};
             f32x4 *dst = reinterpret_cast<f32x4 *>(w.nums + at * D + 4u * NB * g);
 #pragma unroll
-            for (int b = 0; b < NB; ++b) dst[b] = f32x4{v[4 * b], v[4 * b + 1], v[4 * b + 2], v[4 * b + 3]};
+            for (int i = 0; i < NB; ++i) dst[i] = f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
             continue;
         }
         const float inv = x.l[t] == 0.0f ? 0.0f : 1.0f / x.l[t];
-        unsigned char *dst = out.data + ((uint64_t)row.begin + col / a.group) * out.token_stride + (uint64_t)(head * a.group + col % a.group) * out.head_stride;
+        unsigned char *dst = out.data + ((uint64_t)b.row.begin + col / a.group) * out.token_stride + (uint64_t)(b.p.head * a.group + col % a.group) * out.head_stride;
         if constexpr (DT == QP_F32) {
             f32x4 *d4 = reinterpret_cast<f32x4 *>(dst) + NB * g;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) d4[b] = f32x4{v[4 * b] * inv, v[4 * b + 1] * inv, v[4 * b + 2] * inv, v[4 * b + 3] * inv};
+            for (int i = 0; i < NB; ++i) d4[i] = f32x4{v[4 * i] * inv, v[4 * i + 1] * inv, v[4 * i + 2] * inv, v[4 * i + 3] * inv};
         } else {
             u32x2 *d2 = reinterpret_cast<u32x2 *>(dst) + NB * g;
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-                d2[b] = u32x2{at_bf16(v[4 * b] * inv) | (at_bf16(v[4 * b + 1] * inv) << 16),
-                              at_bf16(v[4 * b + 2] * inv) | (at_bf16(v[4 * b + 3] * inv) << 16)};
+            for (int i = 0; i < NB; ++i)
+                d2[i] = u32x2{at_bf16(v[4 * i] * inv) | (at_bf16(v[4 * i + 1] * inv) << 16),
+                              at_bf16(v[4 * i + 2] * inv) | (at_bf16(v[4 * i + 3] * inv) << 16)};
         }
     }
 }
 
-// ---- the pieces of a column, joined: a block a column, every fourth piece a wave ----------------------------------------------
-template <int D, int NCT, int DT> __global__ __launch_bounds__(kAtThreads) void k_kv_join(KvView out, uint32_t q_heads, AtWork w)
+#ifndef QP_KV_FEW_WAVES
+#define QP_KV_FEW_WAVES 2
+#endif
+#ifndef QP_SUB
+#define QP_SUB 2
+#endif
+#ifndef QP_KV_MANY_WAVES
+#define QP_KV_MANY_WAVES 2
+#endif
+template <int D, int DT>
+__global__ __launch_bounds__(kAtThreads, D <= 128 ? QP_KV_FEW_WAVES : 1) void k_kv_attention_few(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
+{
+    using Wave = AtWave<D, 1, DT>;
+    constexpr int NB = Wave::NB;
+    // two waves' numerators and (m, sum) when the four are joined; the grids of each wave's step
+    __shared__ __align__(16) float nums[2][16][D + 4];
+    __shared__ float2 sums[2][16];
+    __shared__ __align__(16) float2 grids[kAtWaves][64];
+    AtBlock b;
+    if (!at_begin<false>(c, a, w, b)) return;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u;
+    const auto slab_at = [&](uint32_t t, bool &there) {
+        const int32_t page = __builtin_amdgcn_readfirstlane(kv_page(c, b.p.row, t >> c.page_shift));
+        there = page >= 0;
+        return kv_slab(c, there ? page : 0, b.p.head);
+    };
+    Wave x;
+    typename Wave::Raw cur, nxt;
+    bool there = false, there_next = false;
+    uint32_t t0 = b.t0 + wave * kAtStep;
+    if (t0 < b.t1) {                          // (on its way while the queries are made ready)
+        const unsigned char *slab = slab_at(t0, there);
+        x.load(cur, slab, t0, c.page_shift, b.row.length, there);
+    }
+    x.load_query(c, qv, a, b.row, b.p.head, b.p.col0, b.p.col1);
+    int32_t sees_lo, sees_hi;
+    at_sees<Wave, 1>(x, sees_lo, sees_hi);
+    const AtMagic magic;
+    for (; t0 < b.t1; t0 += kAtTile) {
+        if (t0 + kAtTile < b.t1) {
+            const unsigned char *slab = slab_at(t0 + kAtTile, there_next);
+            x.load(nxt, slab, t0 + kAtTile, c.page_shift, b.row.length, there_next);
+        }
+        const bool whole = there && (int32_t)t0 >= sees_lo && (int32_t)(t0 + kAtStep) <= sees_hi;
+        x.step_alone(cur, grids[wave], magic, t0, whole, there);
+        cur = nxt;
+        there = there_next;
+    }
+    x.finish();
+#pragma unroll
+    for (uint32_t half = 2; half >= 1; half /= 2) {      // waves 2, 3 into 0, 1, then 1 into 0
+        if (wave >= half && wave < 2u * half) {
+            float *dst = &nums[wave - half][n][4u * NB * g];
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4)
+#pragma unroll
+                for (int i = 0; i < NB; ++i) dst[r4 * NB + i] = x.o[0][i][r4];
+            if (g == 0u) sums[wave - half][n] = float2{x.m[0], x.l[0]};
+        }
+        __syncthreads();
+        if (wave < half) {
+            const float *src = &nums[wave][n][4u * NB * g];
+            const float2 other = sums[wave][n];
+            const float top = fmaxf(x.m[0], other.x), ea = at_exp2(x.m[0] - top), eb = at_exp2(other.x - top);
+            x.m[0] = top;
+            x.l[0] = fmaf(x.l[0], ea, other.y * eb);
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4)
+#pragma unroll
+                for (int i = 0; i < NB; ++i) x.o[0][i][r4] = fmaf(x.o[0][i][r4], ea, src[r4 * NB + i] * eb);
+        }
+        __syncthreads();
+    }
+    if (wave == 0u) at_store<D, 1, DT>(x, b, a, w, out, kAtCols<false>, b.p.col0, b.p.col1);
+}
+
+template <int D, int DT>
+__global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? QP_KV_MANY_WAVES : 1) void k_kv_attention_many(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
+{
+    constexpr int NCT = 2;
+    using Wave = AtWave<D, NCT, DT>;
+    constexpr int NB = Wave::NB, KS = Wave::KS;
+    constexpr uint32_t kFrags = 2 * KS + NB;                        // fragments of 32 tokens: keys (j, k), then values
+    constexpr uint32_t kMine = (kFrags + kAtWaves - 1) / kAtWaves;  // a wave's
+    constexpr uint32_t kSub = D <= 128 ? QP_SUB : 1, kStage = kSub * kAtStep;      // tokens between two barriers
+    struct Stage {
+        f16x8 frags[kFrags][kWave];
+        float2 grids[64];
+    };
+    __shared__ __align__(16) Stage stages[2][kSub];
+    AtBlock b;
+    if (!at_begin<true>(c, a, w, b)) return;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u;
+    const uint32_t col0 = min(b.p.col0 + wave * 16u * NCT, b.p.col1), col1 = min(col0 + 16u * NCT, b.p.col1);
+    const AtMagic magic;
+    // Every wave takes a quarter of a stage's words apart for all of them: while the waves go through a stage, the next one's
+    // fragments go to the other half of LDS and the words of the one after it are on their way.
+    uint32_t words[kSub][kMine];
+    float2 grid[kSub];
+    bool there[3][kSub];                                            // of this stage, the next, the one after
+    const auto fetch = [&](uint32_t t, bool (&is)[kSub]) {
+#pragma unroll
+        for (uint32_t u = 0; u < kSub; ++u) {
+            const uint32_t at = t + u * kAtStep;
+            const int32_t page = at < b.t1 ? __builtin_amdgcn_readfirstlane(kv_page(c, b.p.row, at >> c.page_shift)) : -1;
+            is[u] = page >= 0;
+            const uint32_t pt = 1u << c.page_shift, in = at & (pt - 1u);
+            const uint32_t *kc = reinterpret_cast<const uint32_t *>(kv_slab(c, page < 0 ? 0 : page, b.p.head)), *vc = kc + (size_t)pt * (D / kKvCodes);
+#pragma unroll
+            for (uint32_t i = 0; i < kMine; ++i) {
+                const uint32_t fr = kAtWaves * i + wave;
+                if (fr < 2u * KS)
+                    words[u][i] = kc[(size_t)(in + 8u * (n / 4u) + 4u * (fr / KS) + n % 4u) * (D / kKvCodes) + g * KS + fr % KS];
+                else if (fr < kFrags)
+                    words[u][i] = vc[(size_t)(in / 8u + g) * D + n * NB + (fr - 2u * KS)];
+            }
+            if (wave == u) {
+                const float2 *grids = reinterpret_cast<const float2 *>(vc + (size_t)pt * (D / kKvCodes));
+                grid[u] = grids[(lane < 32u ? 0u : pt) + in + lane % 32u];
+                if (!is[u] || (int32_t)(at + lane % 32u) >= b.row.length) grid[u] = float2{0.0f, 0.0f};
+            }
+        }
+    };
+    const auto put = [&](uint32_t half) {
+#pragma unroll
+        for (uint32_t u = 0; u < kSub; ++u) {
+#pragma unroll
+            for (uint32_t i = 0; i < kMine; ++i) {
+                const uint32_t fr = kAtWaves * i + wave;
+                if (fr < kFrags) stages[half][u].frags[fr][lane] = at_codes(words[u][i], magic);
+            }
+            if (wave == u) stages[half][u].grids[lane] = Wave::centred(grid[u]);
+        }
+    };
+    uint32_t half = 0u;
+    if (b.t0 < b.t1) fetch(b.t0, there[0]);                         // (on their way while the queries are made ready)
+    Wave x;
+    x.load_query(c, qv, a, b.row, b.p.head, col0, col1);
+    int32_t sees_lo, sees_hi;
+    at_sees<Wave, NCT>(x, sees_lo, sees_hi);
+    uint32_t w_lo = 0u, w_hi = 0u;                                  // what any of this wave's columns sees
+    if (col0 < col1) at_range(b.row, a, col0, col1, w_lo, w_hi);
+    if (b.t0 < b.t1) {
+        put(0u);
+        if (b.t0 + kStage < b.t1) fetch(b.t0 + kStage, there[1]);
+    }
+    __syncthreads();
+    for (uint32_t t = b.t0; t < b.t1; t += kStage) {
+        if (t + kStage < b.t1) {
+            put(half ^ 1u);
+            if (t + 2u * kStage < b.t1) fetch(t + 2u * kStage, there[2]);
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kSub; ++u) {
+            const uint32_t at = t + u * kAtStep;
+            if (at + kAtStep > w_lo && at < min(w_hi, b.t1)) {
+                const Stage &st = stages[half][u];
+                const bool whole = there[0][u] && (int32_t)at >= sees_lo && (int32_t)(at + kAtStep) <= sees_hi;
+                x.step([&](int j, int k) { return st.frags[j * KS + k][lane]; }, [&](int i) { return st.frags[2 * KS + i][lane]; }, st.grids, at, whole, there[0][u]);
+            }
+        }
+        __syncthreads();
+        half ^= 1u;
+#pragma unroll
+        for (uint32_t u = 0; u < kSub; ++u) {
+            there[0][u] = there[1][u];
+            there[1][u] = there[2][u];
+        }
+    }
+    x.finish();
+    at_store<D, NCT, DT>(x, b, a, w, out, kAtCols<true>, col0, col1);
+}
+
+// ---- the pieces of a column, joined ----------------------------------------------------------------------------------------
+// Few columns (single tokens, perhaps of very long rows): a block a column, every fourth piece a wave.  Many: a wave a column.
+constexpr uint32_t kAtJoinBlocks = 2048, kAtJoinFew = 2048;
+template <int D, int DT> __device__ __forceinline__ void at_answer(const KvView &out, uint32_t q_heads, uint32_t place, uint32_t d, float v)
+{
+    unsigned char *dst = out.data + (uint64_t)(place / q_heads) * out.token_stride + (uint64_t)(place % q_heads) * out.head_stride;
+    if constexpr (DT == QP_F32) reinterpret_cast<float *>(dst)[d] = v;
+    else reinterpret_cast<uint16_t *>(dst)[d] = (uint16_t)at_bf16(v);
+}
+__device__ __forceinline__ float at_wave_sum(float v)
+{
+    v += dpp_f32<kDppQuadSwap1>(v);
+    v += dpp_f32<kDppQuadSwap2>(v);
+    v += dpp_f32<kDppHalfMirror>(v);
+    v += dpp_f32<kDppRowMirror>(v);
+    v += kv_xor_f32(v, 16);
+    return v + kv_xor_f32(v, 32);
+}
+template <int D, int DT> __global__ __launch_bounds__(kAtThreads) void k_kv_join(KvView out, uint32_t q_heads, AtWork few, AtWork many)
 {
     constexpr int PER = (D + kWave - 1) / kWave;
-    __shared__ float weight[2 * kAtTarget<NCT>];
+    constexpr uint32_t kMost = 2u * (kAtTarget<false> > kAtTarget<true> ? kAtTarget<false> : kAtTarget<true>);
+    __shared__ float weight[kMost];
     __shared__ float part[kAtWaves][D], top_of[kAtWaves], sum_of[kAtWaves];
     const uint32_t tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
-    const uint32_t count = w.header[0];
+    const uint32_t first = few.most_cols ? few.header[0] : 0u, count = first + (many.most_cols ? many.header[0] : 0u);
+    if (count > kAtJoinFew) {
+        for (uint32_t k = blockIdx.x * kAtWaves + wave; k < count; k += gridDim.x * kAtWaves) {
+            const AtWork &w = k < first ? few : many;
+            const u32x4 rec = w.cols[k < first ? k : k - first];
+            const uint32_t pieces = rec[1];
+            if (pieces == 0u) continue;       // its item came out in one piece after all
+            float top = -3.402823466e38f, sum = 0.0f, acc[PER];
+            for (uint32_t i = lane; i < pieces; i += kWave) top = fmaxf(top, w.sums[rec[0] + (size_t)i * rec[2]].x);
+            top = wave_max(top);
+#pragma unroll
+            for (int z = 0; z < PER; ++z) acc[z] = 0.0f;
+            for (uint32_t i0 = 0; i0 < pieces; i0 += kWave) {
+                float e = 0.0f;
+                if (i0 + lane < pieces) {
+                    const float2 ml = w.sums[rec[0] + (size_t)(i0 + lane) * rec[2]];
+                    e = at_exp2(ml.x - top);
+                    sum = fmaf(e, ml.y, sum);
+                }
+                const uint32_t n = min((uint32_t)kWave, pieces - i0);
+                for (uint32_t i = 0; i < n; ++i) {
+                    const float *src = w.nums + (rec[0] + (size_t)(i0 + i) * rec[2]) * D;
+                    const float f = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e), i));
+#pragma unroll
+                    for (int z = 0; z < PER; ++z)
+                        if (lane + kWave * z < (uint32_t)D) acc[z] = fmaf(f, src[lane + kWave * z], acc[z]);
+                }
+            }
+            sum = at_wave_sum(sum);
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+            for (int z = 0; z < PER; ++z)
+                if (lane + kWave * z < (uint32_t)D) at_answer<D, DT>(out, q_heads, rec[3], lane + kWave * z, acc[z] * inv);
+        }
+        return;
+    }
     for (uint32_t k = blockIdx.x; k < count; k += gridDim.x) {
-        const u32x4 rec = w.cols[k];
+        const AtWork &w = k < first ? few : many;
+        const u32x4 rec = w.cols[k < first ? k : k - first];
         const uint32_t pieces = rec[1];
-        if (pieces == 0u) continue;           // its item came out in one piece after all
+        if (pieces == 0u) continue;
         float top = -3.402823466e38f;
         for (uint32_t i = tid; i < pieces; i += kAtThreads) top = fmaxf(top, w.sums[rec[0] + (size_t)i * rec[2]].x);
         top = wave_max(top);
@@ -761,19 +868,14 @@ template <int D, int NCT, int DT> __global__ __launch_bounds__(kAtThreads) void 
             const float2 ml = w.sums[rec[0] + (size_t)i * rec[2]];
             const float e = at_exp2(ml.x - top);
             weight[i] = e;
-            sum += e * ml.y;
+            sum = fmaf(e, ml.y, sum);
         }
-        sum += dpp_f32<kDppQuadSwap1>(sum);
-        sum += dpp_f32<kDppQuadSwap2>(sum);
-        sum += dpp_f32<kDppHalfMirror>(sum);
-        sum += dpp_f32<kDppRowMirror>(sum);
-        sum += kv_xor_f32(sum, 16);
-        sum += kv_xor_f32(sum, 32);
+        sum = at_wave_sum(sum);
         if (lane == 0u) sum_of[wave] = sum;
         __syncthreads();
         float acc[PER];
 #pragma unroll
-        for (int e = 0; e < PER; ++e) acc[e] = 0.0f;
+        for (int z = 0; z < PER; ++z) acc[z] = 0.0f;
 #pragma unroll 4
         for (uint32_t i = wave; i < pieces; i += kAtWaves) {
             const float *src = w.nums + (rec[0] + (size_t)i * rec[2]) * D;
@@ -788,39 +890,38 @@ template <int D, int NCT, int DT> __global__ __launch_bounds__(kAtThreads) void 
         __syncthreads();
         const float l = (sum_of[0] + sum_of[1]) + (sum_of[2] + sum_of[3]);
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        unsigned char *dst = out.data + (uint64_t)(rec[3] / q_heads) * out.token_stride + (uint64_t)(rec[3] % q_heads) * out.head_stride;
-        for (uint32_t d = tid; d < (uint32_t)D; d += kAtThreads) {
-            const float v = ((part[0][d] + part[1][d]) + (part[2][d] + part[3][d])) * inv;
-            if constexpr (DT == QP_F32) reinterpret_cast<float *>(dst)[d] = v;
-            else reinterpret_cast<uint16_t *>(dst)[d] = (uint16_t)at_bf16(v);
-        }
+        for (uint32_t d = tid; d < (uint32_t)D; d += kAtThreads)
+            at_answer<D, DT>(out, q_heads, rec[3], d, ((part[0][d] + part[1][d]) + (part[2][d] + part[3][d])) * inv);
         __syncthreads();                      // (the shared arrays are used again)
     }
 }
 
-template <int D, int NCT, int DT>
-static hipError_t at_launch(const KvLayer &c, const KvView &q, const KvView &out, const KvAttn &a, void *ws, hipStream_t s)
+template <int D, int DT>
+static hipError_t at_launch(const KvLayer &c, const KvView &q, const KvView &out, const KvAttn &a, char *ws, hipStream_t s)
 {
-    size_t bytes;
-    const AtWork w = at_work<NCT>(ws, c, D, a.group, bytes);
-    // kAtTarget pieces and one more for each item at most
-    const unsigned blocks = (unsigned)(kAtTarget<NCT> + at_items(NCT, c, a.group));
-    hipLaunchKernelGGL((k_kv_attention<D, NCT, DT>), dim3(blocks), dim3(kAtThreads), 0, s, c, q, out, a, w);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || w.most_cols == 0u) return e;      // (no row is longer than a piece)
-    hipLaunchKernelGGL((k_kv_join<D, NCT, DT>), dim3(w.most_cols < 2048u ? w.most_cols : 2048u), dim3(kAtThreads), 0, s, out, c.kv_heads * a.group, w);
+    const bool wide = at_wide(a.group, c.rows, c.tokens);
+    size_t few_bytes, bytes;
+    (void)at_bytes(c, D, a.group, few_bytes);
+    const AtWork few = at_work<false>(ws, c, D, a.group, bytes);
+    const AtWork many = wide ? at_work<true>(ws + few_bytes, c, D, a.group, bytes) : AtWork{};
+    // the target's pieces, and one more for each item at most
+    hipError_t e;
+    if (wide) {
+        hipLaunchKernelGGL((k_kv_attention_many<D, DT>), dim3((unsigned)(kAtTarget<true> + at_items<true>(c, a.group))), dim3(kAtThreads), 0, s, c, q, out, a, many);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((k_kv_attention_few<D, DT>), dim3((unsigned)(kAtTarget<false> + at_items<false>(c, a.group))), dim3(kAtThreads), 0, s, c, q, out, a, few);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const uint32_t cols = few.most_cols + many.most_cols;
+    if (cols == 0u) return hipSuccess;        // no row is longer than a piece
+    hipLaunchKernelGGL((k_kv_join<D, DT>), dim3(cols < kAtJoinBlocks ? cols : kAtJoinBlocks), dim3(kAtThreads), 0, s, out, c.kv_heads * a.group, few, many);
     return hipGetLastError();
 }
 
-// Columns that a wave takes, 16 NCT: 16 where rows bring no more than that on average (single tokens), else 32: a word of codes, once
-// taken apart, serves twice as many.
-inline bool at_narrow(uint32_t group, uint32_t rows, uint64_t tokens) { return tokens * group <= 16ull * rows; }
-
 template <int D> hipError_t at_dim(const KvLayer &c, int dtype, const KvView &q, const KvView &out, const KvAttn &a, void *ws, hipStream_t s)
 {
-    if (at_narrow(a.group, c.rows, c.tokens))
-        return dtype == QP_F32 ? at_launch<D, 1, QP_F32>(c, q, out, a, ws, s) : at_launch<D, 1, QP_BF16>(c, q, out, a, ws, s);
-    return dtype == QP_F32 ? at_launch<D, 2, QP_F32>(c, q, out, a, ws, s) : at_launch<D, 2, QP_BF16>(c, q, out, a, ws, s);
+    char *p = static_cast<char *>(ws);
+    return dtype == QP_F32 ? at_launch<D, QP_F32>(c, q, out, a, p, s) : at_launch<D, QP_BF16>(c, q, out, a, p, s);
 }
 #define QP_KV_ATTENTION_DIM(D) \
     template hipError_t at_dim<D>(const KvLayer &, int, const KvView &, const KvView &, const KvAttn &, void *, hipStream_t)

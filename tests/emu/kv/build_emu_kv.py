@@ -1,5 +1,5 @@
 """TEST INFRASTRUCTURE ONLY: compiles the 4-bit key/value cache's kernels and C ABI against the CPU stand-in for the HIP runtime,
-with AddressSanitizer and UBSan, into tests/emu/_build/kv/emu_kv_driver.  A call is cut into few pieces (QP_KV_TARGET), so
+with AddressSanitizer and UBSan, into tests/emu/_build/kv/emu_kv_driver.  A call is cut into few pieces (QP_KV_FEW, QP_KV_MANY), so
 that a launch is a handful of emulated blocks and small contexts are still split and joined."""
 from __future__ import annotations
 
@@ -14,7 +14,7 @@ EMU = os.path.dirname(HERE)
 sys.path.insert(0, EMU)
 import build_emu  # noqa: E402
 
-FLAGS = ["-DQP_KV_TARGET=12", "-DQP_KV_LEAST=1", "-DQP_KV_COPY_BLOCKS=4"]
+FLAGS = ["-DQP_KV_FEW=12", "-DQP_KV_MANY=9", "-DQP_KV_LEAST=1", "-DQP_KV_COPY_BLOCKS=4"]
 
 
 def build():
