@@ -232,6 +232,23 @@ template <bool MANY> __device__ __forceinline__ bool at_find(const KvLayer &c, c
     return have != 0u;
 }
 
+// The pages of a row, 64 at a time: lane i has slot base + i's.  (A load for each would be waited for in each step: 600 cycles.)
+struct AtPages {
+    int32_t page;
+    uint32_t base;
+    __device__ __forceinline__ void load(const KvLayer &c, uint32_t row, uint32_t slot)
+    {
+        base = slot;
+        page = kv_page(c, row, slot + threadIdx.x % kWave);
+    }
+    // the page of slot `slot`, which is the same in all lanes and never below an earlier call's
+    __device__ __forceinline__ int32_t at(const KvLayer &c, uint32_t row, uint32_t slot)
+    {
+        if (slot - base >= (uint32_t)kWave) load(c, row, slot);
+        return __builtin_amdgcn_readlane(page, (int)(slot - base));
+    }
+};
+
 // ---- a wave's work -----------------------------------------------------------------------------------------------------------
 // The constants of at_codes in vector registers: (w & mask) | magic is one instruction then (it takes one scalar operand only),
 // and two with the constants in it.
@@ -270,6 +287,7 @@ template <int D, int NCT, int DT> struct AtWave {
     struct Raw {
         uint32_t k[2][KS], v[NB];
         float2 grid;                                 // lanes 0..31: keys, 32..63: values
+        bool written;                                // else the grid may be anything (looked at when it is used: not to wait for it before)
     };
 
     __device__ __forceinline__ void load_query(const KvLayer &c, const KvView &qv, const KvAttn &a, const KvRow &row, uint32_t head,
@@ -349,20 +367,27 @@ template <int D, int NCT, int DT> struct AtWave {
         sv_most = 0.0f;
     }
 
+    // Where a lane's words and grid of 32 tokens lie, in bytes from the head's slab + (first token's slot) * D / 2 (the grid: + 8 of the
+    // slot): codes of a token are D / 2 bytes and so is an eighth of eight tokens' values.
+    uint32_t key_at, value_at, grid_at;
+    __device__ __forceinline__ void place(uint32_t page_shift)
+    {
+        const uint32_t lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u, pt = 1u << page_shift;
+        key_at = (8u * (n / 4u) + n % 4u) * (D / 2) + g * KS * 4u;
+        value_at = pt * (D / 2) + (g * D + n * NB) * 4u;
+        grid_at = pt * D + (lane < 32u ? 0u : pt * 8u) + lane % 32u * 8u;
+    }
     // 32 tokens from `t0` on, of the page that they all lie in
     __device__ __forceinline__ void load(Raw &x, const unsigned char *slab, uint32_t t0, uint32_t page_shift, int32_t length, bool there) const
     {
-        const uint32_t lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u;
-        const uint32_t pt = 1u << page_shift, in = t0 & (pt - 1u);
-        const uint32_t *kc = reinterpret_cast<const uint32_t *>(slab);
-        const uint32_t *vc = kc + (size_t)pt * (D / kKvCodes);
-        const float2 *grids = reinterpret_cast<const float2 *>(vc + (size_t)pt * (D / kKvCodes));
+        const uint32_t in = t0 & ((1u << page_shift) - 1u);
+        const unsigned char *codes = slab + (size_t)in * (D / 2);
 #pragma unroll
         for (int j = 0; j < 2; ++j)      // (the last words of a key that is no multiple of 32 long lie behind it, in the slab; their queries are 0)
-            __builtin_memcpy(x.k[j], kc + (size_t)(in + 8u * (n / 4u) + 4u * j + n % 4u) * (D / kKvCodes) + g * KS, sizeof x.k[j]);
-        __builtin_memcpy(x.v, vc + (size_t)(in / 8u + g) * D + n * NB, sizeof x.v);
-        x.grid = grids[(lane < 32u ? 0u : pt) + in + lane % 32u];
-        if (!there || (int32_t)(t0 + lane % 32u) >= length) x.grid = float2{0.0f, 0.0f};   // (never written: may be anything)
+            __builtin_memcpy(x.k[j], codes + key_at + 4u * j * (D / 2), sizeof x.k[j]);
+        __builtin_memcpy(x.v, codes + value_at, sizeof x.v);
+        x.grid = *reinterpret_cast<const float2 *>(slab + (size_t)in * 8u + grid_at);
+        x.written = there && (int32_t)(t0 + threadIdx.x % 32u) < length;
     }
 
     // the maximum or N moves
@@ -396,7 +421,10 @@ template <int D, int NCT, int DT> struct AtWave {
     }
 
     // What a step makes of a grid; lanes 0..31: keys, 32..63: values.
-    static __device__ __forceinline__ float2 centred(float2 grid) { return float2{grid.y, fmaf(8.0f, grid.y, grid.x)}; }
+    static __device__ __forceinline__ float2 centred(float2 grid, bool written)
+    {
+        return written ? float2{grid.y, fmaf(8.0f, grid.y, grid.x)} : float2{0.0f, 0.0f};
+    }
 
     // `key(j, k)`, `value(b)`: the fragments; `mem`: scales and lo + 8 scale of 32 keys, then of 32 values
     template <typename Key, typename Value>
@@ -488,7 +516,7 @@ template <int D, int NCT, int DT> struct AtWave {
     // One wave for itself: 32 tokens that it has loaded.  `mem`: this wave's own.
     __device__ __forceinline__ void step_alone(const Raw &x, float2 *mem, const AtMagic &magic, uint32_t t0, bool whole, bool there)
     {
-        mem[threadIdx.x % kWave] = centred(x.grid);
+        mem[threadIdx.x % kWave] = centred(x.grid, x.written);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         step([&](int j, int k) { return at_codes(x.k[j][k], magic); }, [&](int b) { return at_codes(x.v[b], magic); }, mem, t0, whole, there);
@@ -639,8 +667,9 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 ? QP_KV_FEW_WAVES : 1) void k_
     AtBlock b;
     if (!at_begin<false>(c, a, w, b)) return;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u;
+    AtPages pages;
     const auto slab_at = [&](uint32_t t, bool &there) {
-        const int32_t page = __builtin_amdgcn_readfirstlane(kv_page(c, b.p.row, t >> c.page_shift));
+        const int32_t page = pages.at(c, b.p.row, t >> c.page_shift);
         there = page >= 0;
         return kv_slab(c, there ? page : 0, b.p.head);
     };
@@ -648,6 +677,8 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 ? QP_KV_FEW_WAVES : 1) void k_
     typename Wave::Raw cur, nxt;
     bool there = false, there_next = false;
     uint32_t t0 = b.t0 + wave * kAtStep;
+    x.place(c.page_shift);
+    pages.load(c, b.p.row, t0 >> c.page_shift);
     if (t0 < b.t1) {                          // (on its way while the queries are made ready)
         const unsigned char *slab = slab_at(t0, there);
         x.load(cur, slab, t0, c.page_shift, b.row.length, there);
@@ -717,28 +748,30 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? QP_KV_MANY_
     // fragments go to the other half of LDS and the words of the one after it are on their way.
     uint32_t words[kSub][kMine];
     float2 grid[kSub];
+    bool written[kSub];
     bool there[3][kSub];                                            // of this stage, the next, the one after
+    // where this lane's words of 32 tokens lie, as in AtWave::place
+    uint32_t word_at[kMine];
+#pragma unroll
+    for (uint32_t i = 0; i < kMine; ++i) {
+        const uint32_t fr = kAtWaves * i + wave;
+        word_at[i] = fr < 2u * KS ? (8u * (n / 4u) + 4u * (fr / KS) + n % 4u) * (D / 2) + (g * KS + fr % KS) * 4u
+                                  : (D / 2 << c.page_shift) + (g * D + n * NB + (fr < kFrags ? fr - 2u * KS : 0u)) * 4u;
+    }
+    const uint32_t grid_at = (D << c.page_shift) + (lane < 32u ? 0u : 8u << c.page_shift) + lane % 32u * 8u;
+    AtPages pages;
+    pages.load(c, b.p.row, b.t0 >> c.page_shift);
     const auto fetch = [&](uint32_t t, bool (&is)[kSub]) {
 #pragma unroll
         for (uint32_t u = 0; u < kSub; ++u) {
-            const uint32_t at = t + u * kAtStep;
-            const int32_t page = at < b.t1 ? __builtin_amdgcn_readfirstlane(kv_page(c, b.p.row, at >> c.page_shift)) : -1;
+            const uint32_t at = t + u * kAtStep, in = at & ((1u << c.page_shift) - 1u);
+            const int32_t page = at < b.t1 ? pages.at(c, b.p.row, at >> c.page_shift) : -1;
             is[u] = page >= 0;
-            const uint32_t pt = 1u << c.page_shift, in = at & (pt - 1u);
-            const uint32_t *kc = reinterpret_cast<const uint32_t *>(kv_slab(c, page < 0 ? 0 : page, b.p.head)), *vc = kc + (size_t)pt * (D / kKvCodes);
+            const unsigned char *slab = kv_slab(c, page < 0 ? 0 : page, b.p.head), *codes = slab + (size_t)in * (D / 2);
 #pragma unroll
-            for (uint32_t i = 0; i < kMine; ++i) {
-                const uint32_t fr = kAtWaves * i + wave;
-                if (fr < 2u * KS)
-                    words[u][i] = kc[(size_t)(in + 8u * (n / 4u) + 4u * (fr / KS) + n % 4u) * (D / kKvCodes) + g * KS + fr % KS];
-                else if (fr < kFrags)
-                    words[u][i] = vc[(size_t)(in / 8u + g) * D + n * NB + (fr - 2u * KS)];
-            }
-            if (wave == u) {
-                const float2 *grids = reinterpret_cast<const float2 *>(vc + (size_t)pt * (D / kKvCodes));
-                grid[u] = grids[(lane < 32u ? 0u : pt) + in + lane % 32u];
-                if (!is[u] || (int32_t)(at + lane % 32u) >= b.row.length) grid[u] = float2{0.0f, 0.0f};
-            }
+            for (uint32_t i = 0; i < kMine; ++i) words[u][i] = *reinterpret_cast<const uint32_t *>(codes + word_at[i]);
+            if (wave == u) grid[u] = *reinterpret_cast<const float2 *>(slab + (size_t)in * 8u + grid_at);
+            written[u] = is[u] && (int32_t)(at + lane % 32u) < b.row.length;
         }
     };
     const auto put = [&](uint32_t half) {
@@ -749,7 +782,7 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? QP_KV_MANY_
                 const uint32_t fr = kAtWaves * i + wave;
                 if (fr < kFrags) stages[half][u].frags[fr][lane] = at_codes(words[u][i], magic);
             }
-            if (wave == u) stages[half][u].grids[lane] = Wave::centred(grid[u]);
+            if (wave == u) stages[half][u].grids[lane] = Wave::centred(grid[u], written[u]);
         }
     };
     uint32_t half = 0u;
