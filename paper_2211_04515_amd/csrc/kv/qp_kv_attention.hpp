@@ -732,7 +732,6 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? QP_KV_MANY_
     using Wave = AtWave<D, NCT, DT>;
     constexpr int NB = Wave::NB, KS = Wave::KS;
     constexpr uint32_t kFrags = 2 * KS + NB;                        // fragments of 32 tokens: keys (j, k), then values
-    constexpr uint32_t kMine = (kFrags + kAtWaves - 1) / kAtWaves;  // a wave's
     constexpr uint32_t kSub = D <= 128 ? QP_SUB : 1, kStage = kSub * kAtStep;      // tokens between two barriers
     struct Stage {
         f16x8 frags[kFrags][kWave];
@@ -745,45 +744,50 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? QP_KV_MANY_
     const uint32_t col0 = min(b.p.col0 + wave * 16u * NCT, b.p.col1), col1 = min(col0 + 16u * NCT, b.p.col1);
     const AtMagic magic;
     // Every wave takes a quarter of a stage's words apart for all of them: while the waves go through a stage, the next one's
-    // fragments go to the other half of LDS and the words of the one after it are on their way.
-    uint32_t words[kSub][kMine];
-    float2 grid[kSub];
-    bool written[kSub];
+    // fragments go to the other half of LDS and the words of the one after it are on their way.  A wave has one of the two tiles of
+    // keys and half of the values of 32 tokens, each one load (of heads of 256 either a tile of keys or half of the values: the stage
+    // is 32 tokens then): with a load for each fragment, attend_prompt took 402 us, so ATTEND_PROMPT.
+    constexpr int kHalf = (NB + 1) / 2;
+    const uint32_t mine = kSub == 2u ? wave / 2u : 0u, side = wave % 2u;
+    const bool keys = kSub == 2u || wave < 2u, values = kSub == 2u || wave >= 2u;
+    uint32_t wk[KS], wv[kHalf];
+    float2 grid{0.0f, 0.0f};
+    bool written = false;
     bool there[3][kSub];                                            // of this stage, the next, the one after
     // where this lane's words of 32 tokens lie, as in AtWave::place
-    uint32_t word_at[kMine];
-#pragma unroll
-    for (uint32_t i = 0; i < kMine; ++i) {
-        const uint32_t fr = kAtWaves * i + wave;
-        word_at[i] = fr < 2u * KS ? (8u * (n / 4u) + 4u * (fr / KS) + n % 4u) * (D / 2) + (g * KS + fr % KS) * 4u
-                                  : (D / 2 << c.page_shift) + (g * D + n * NB + (fr < kFrags ? fr - 2u * KS : 0u)) * 4u;
-    }
+    const uint32_t key_at = (8u * (n / 4u) + 4u * side + n % 4u) * (D / 2) + g * KS * 4u;
+    const uint32_t value_at = (D / 2 << c.page_shift) + (g * D + n * NB + side * kHalf) * 4u;
     const uint32_t grid_at = (D << c.page_shift) + (lane < 32u ? 0u : 8u << c.page_shift) + lane % 32u * 8u;
     AtPages pages;
     pages.load(c, b.p.row, b.t0 >> c.page_shift);
     const auto fetch = [&](uint32_t t, bool (&is)[kSub]) {
+        int32_t page = -1;
 #pragma unroll
         for (uint32_t u = 0; u < kSub; ++u) {
-            const uint32_t at = t + u * kAtStep, in = at & ((1u << c.page_shift) - 1u);
-            const int32_t page = at < b.t1 ? pages.at(c, b.p.row, at >> c.page_shift) : -1;
-            is[u] = page >= 0;
-            const unsigned char *slab = kv_slab(c, page < 0 ? 0 : page, b.p.head), *codes = slab + (size_t)in * (D / 2);
-#pragma unroll
-            for (uint32_t i = 0; i < kMine; ++i) words[u][i] = *reinterpret_cast<const uint32_t *>(codes + word_at[i]);
-            if (wave == u) grid[u] = *reinterpret_cast<const float2 *>(slab + (size_t)in * 8u + grid_at);
-            written[u] = is[u] && (int32_t)(at + lane % 32u) < b.row.length;
+            const uint32_t at = t + u * kAtStep;
+            const int32_t p = at < b.t1 ? pages.at(c, b.p.row, at >> c.page_shift) : -1;
+            is[u] = p >= 0;
+            if (u == mine) page = p;
         }
+        const uint32_t at = t + mine * kAtStep, in = at & ((1u << c.page_shift) - 1u);
+        const unsigned char *slab = kv_slab(c, page < 0 ? 0 : page, b.p.head), *codes = slab + (size_t)in * (D / 2);
+        if (keys) __builtin_memcpy(wk, codes + key_at, sizeof wk);
+        if (values) __builtin_memcpy(wv, codes + value_at, sizeof wv);   // (an odd number of blocks: the last word is not this head's, and not used)
+        if (side == 0u && keys) grid = *reinterpret_cast<const float2 *>(slab + (size_t)in * 8u + grid_at);
+        written = page >= 0 && (int32_t)(at + lane % 32u) < b.row.length;
     };
     const auto put = [&](uint32_t half) {
+        Stage &st = stages[half][mine];
+        if (keys) {
 #pragma unroll
-        for (uint32_t u = 0; u < kSub; ++u) {
-#pragma unroll
-            for (uint32_t i = 0; i < kMine; ++i) {
-                const uint32_t fr = kAtWaves * i + wave;
-                if (fr < kFrags) stages[half][u].frags[fr][lane] = at_codes(words[u][i], magic);
-            }
-            if (wave == u) stages[half][u].grids[lane] = Wave::centred(grid[u], written[u]);
+            for (uint32_t k = 0; k < (uint32_t)KS; ++k) st.frags[side * KS + k][lane] = at_codes(wk[k], magic);
         }
+        if (values) {
+#pragma unroll
+            for (uint32_t i = 0; i < (uint32_t)kHalf; ++i)
+                if (NB % 2 == 0 || side * kHalf + i < (uint32_t)NB) st.frags[2 * KS + side * kHalf + i][lane] = at_codes(wv[i], magic);
+        }
+        if (side == 0u && keys) st.grids[lane] = Wave::centred(grid, written);
     };
     uint32_t half = 0u;
     if (b.t0 < b.t1) fetch(b.t0, there[0]);                         // (on their way while the queries are made ready)
