@@ -7,9 +7,8 @@
 // the second term the same for all elements of a head.  So both products run on the codes themselves: c - 8 is an integer in
 // [-8, 7], exact in fp16, and no value is ever dequantized.  (Centred codes, because the rounding of p_t s_t is multiplied by
 // them: -8..7 costs about as much as the values' own spread would.)
-//   q          is scaled by a power of two per column so that its largest element lies in [2^14, 2^15) and taken as fp16:
-//              exact for bf16 (elements below 2^-30 of the largest aside, which round at 2^-39 of it); fp32 is split in two
-//              halves, 22 bits of each element.
+//   q          is taken as 16 q in fp16: exact for bf16 (what is below 2^-14 rounds at 2^-29); fp32 is split in two halves, 22 bits
+//              of each element.  A column whose largest element lies outside [2^-4, 2^11) gets a power of two of its own.
 //   p_t s_t    is rounded to fp16 (fp32: split in two).  s_t is normalised by a power of two N so that the largest one seen lies
 //              in [2^5, 2^7], and p_t <= 2^8, so that nothing overflows and what is lost at the lower end is 2^-32 of the largest.
 //   Scores, the running maximum m, sum p_t, sum p_t (lo_t + 8 s_t) and the accumulators are fp32.
@@ -22,7 +21,8 @@
 // A word w becomes eight halves as ((w >> 8 i) & 0x000f000f | 0x6400 6400) - 1032 and (.. & 0x00f000f0 | 0x5400 5400) - 72: codes
 // 0, 4, 1, 5, 2, 6, 3, 7; queries and p are put in the same order.
 // The maximum is lazy: a column's m moves only when a lane sees a score more than 8 (in log2) above it, so the loop has no exchange
-// between lanes; what is rare (the maximum moves, N moves) is one branch of the whole wave.
+// between lanes; what is rare (the maximum moves, N moves) is one branch of the whole wave.  Scores are made relative to m in the step
+// that applies the grid, with scale log2(e) / 16 in the grid already: two instructions for a score, and the exponential's argument is there.
 //
 // Who does what.  An item is some columns of one row and key head, a block (four waves) takes an item or a piece of its tokens:
 //   few    16 columns; every wave all of them and every fourth 32 tokens, joined through LDS at the end.  What a single token of a
@@ -279,7 +279,10 @@ template <int D, int NCT, int DT> struct AtWave {
     static constexpr int PIECES = DT == QP_F32 ? 2 : 1;
     f16x8 q[NCT][PIECES][KS];
     f32x4 o[NCT][NB];
-    float m[NCT], f[NCT], bq[NCT], l[NCT], lv[NCT];
+    float m[NCT], bq[NCT], l[NCT], lv[NCT];          // m in log2
+    float over[NCT];                                 // above it a score moves m: the headroom, or -inf while nothing was seen
+    float own[NCT];                                  // the column's own power of two
+    bool owns;                                       // any column of the wave has one
     int32_t lo[NCT], hi[NCT];                        // the tokens that this lane's column sees
     float norm, sv_most;                             // N, and the largest value scale that it is good for
     int32_t norm_exp;
@@ -331,9 +334,14 @@ template <int D, int NCT, int DT> struct AtWave {
             uint32_t any = bad ? 1u : 0u;
             any |= __shfl_xor(any, 16, kWave);
             any |= __shfl_xor(any, 32, kWave);
-            int32_t ex = 15;
-            if (top > 0.0f && any == 0u) (void)frexpf(top, &ex);
-            const int32_t up = min(15 - ex, 100);        // q 2^up: the largest element in [2^14, 2^15)
+            int32_t up = 4;
+            if (top != 0.0f && any == 0u && !(top >= 0x1p-4f && top < 0x1p11f)) {
+                int32_t ex;
+                (void)frexpf(top, &ex);
+                up = min(15 - ex, 100);                  // q 2^up: the largest element in [2^14, 2^15)
+            }
+            own[t] = ldexpf(1.0f, 4 - up);
+            owns = (t != 0 && owns) || __ballot(up != 4) != 0ull;
             float sum = 0.0f;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
@@ -351,10 +359,9 @@ template <int D, int NCT, int DT> struct AtWave {
             }
             sum += kv_xor_f32(sum, 16);
             sum += kv_xor_f32(sum, 32);
-            bq[t] = any ? __uint_as_float(0x7fc00000u) : sum;
-            // f > 0, and m f finite from the start: a masked score, -inf, gives p = 0 by itself
-            f[t] = fmaxf(ldexpf(a.scale * 1.44269504088896341f, -up), 0x1p-126f);
-            m[t] = -0x1p127f / fmaxf(f[t], 1.0f);
+            bq[t] = any ? __uint_as_float(0x7fc00000u) : sum * own[t];
+            m[t] = 0.0f;
+            over[t] = -INFINITY;
             l[t] = lv[t] = 0.0f;
 #pragma unroll
             for (int b = 0; b < NB; ++b) o[t][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -390,8 +397,9 @@ template <int D, int NCT, int DT> struct AtWave {
         x.written = there && (int32_t)(t0 + threadIdx.x % 32u) < length;
     }
 
-    // the maximum or N moves
-    __device__ __forceinline__ void rescale(const float (&top)[NCT], float sv_top)
+    // The maximum or N moves.
+    // `s`: scores relative to m, which follow
+    template <int SUB> __device__ __forceinline__ void rescale(f32x4 (&s)[SUB][NCT][2], const float (&top)[NCT], float sv_top)
     {
         sv_top = fmaxf(sv_top, kv_xor_f32(sv_top, 16));
         sv_top = fmaxf(sv_top, kv_xor_f32(sv_top, 32));
@@ -409,117 +417,160 @@ template <int D, int NCT, int DT> struct AtWave {
         for (int t = 0; t < NCT; ++t) {
             float x = fmaxf(top[t], kv_xor_f32(top[t], 16));
             x = fmaxf(x, kv_xor_f32(x, 32));
-            const float next = fmaxf(m[t], x);
-            const float alpha = at_exp2((m[t] - next) * f[t]);
-            m[t] = next;
+            const bool first = over[t] < 0.0f;
+            const float up = x == -INFINITY ? 0.0f : first ? x : fmaxf(x, 0.0f);     // (x NaN: 0 or NaN; the column is lost anyway)
+            over[t] = x == -INFINITY ? over[t] : kAtHeadroom;
+            const float alpha = first ? 1.0f : at_exp2(-up);                          // (first: there is nothing to scale)
+            m[t] += up;
             l[t] *= alpha;
             lv[t] *= alpha;
             const float beta = alpha * ratio;
 #pragma unroll
             for (int b = 0; b < NB; ++b) o[t][b] *= beta;
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                s[u][t][0] -= up;
+                s[u][t][1] -= up;
+            }
         }
     }
 
-    // What a step makes of a grid; lanes 0..31: keys, 32..63: values.
-    static __device__ __forceinline__ float2 centred(float2 grid, bool written)
+    // What a step makes of a grid: {scale, lo + 8 scale}; those of keys (lanes 0..31, values 32..63) with the scores' factor.
+    static __device__ __forceinline__ float2 centred(float2 grid, bool written, float key_factor)
     {
-        return written ? float2{grid.y, fmaf(8.0f, grid.y, grid.x)} : float2{0.0f, 0.0f};
+        const float f = threadIdx.x % kWave < 32u ? key_factor : 1.0f;
+        return written ? float2{grid.y * f, fmaf(8.0f, grid.y, grid.x) * f} : float2{0.0f, 0.0f};
     }
 
-    // `key(j, k)`, `value(b)`: the fragments; `mem`: scales and lo + 8 scale of 32 keys, then of 32 values
-    template <typename Key, typename Value>
-    __device__ __forceinline__ void step(const Key &key, const Value &value, const float2 *mem, uint32_t t0, bool whole, bool there)
+    // Scores of 32 SUB tokens, before the grids: the first product.  `key(u, j, k)`: the fragments.
+    template <int SUB> struct Scores {
+        f32x4 s[SUB][NCT][2];
+    };
+    template <int SUB, typename Key> __device__ __forceinline__ void products(Scores<SUB> &x, const Key &key) const
+    {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+#pragma unroll
+            for (int t = 0; t < NCT; ++t) x.s[u][t][0] = x.s[u][t][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    const f16x8 a = key(u, j, k);
+#pragma unroll
+                    for (int t = 0; t < NCT; ++t)
+#pragma unroll
+                        for (int z = PIECES - 1; z >= 0; --z) x.s[u][t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, q[t][z][k], x.s[u][t][j], 0, 0, 0);
+                }
+        }
+    }
+    // The rest of a step: softmax and the second product.  `value(u, b)`: the fragments; `mem(u)`: scales and lo + 8 scale of 32 keys, then of
+    // 32 values; `there(u)`: the page is.
+    template <int SUB, typename Value, typename Mem, typename There>
+    __device__ __forceinline__ void weigh(Scores<SUB> &x, const Value &value, const Mem &mem, uint32_t t0, bool whole, const There &there)
     {
         const uint32_t lane = threadIdx.x % kWave, g = lane / 16u;
-        float sk[8], bk[8], sv[8], bv[8];                 // of tokens 8 g + i
+        float top[NCT], sv_top = 0.0f;
+        if (owns) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 gk = mem[8u * g + i], gv = mem[32u + 8u * g + i];
-            sk[i] = gk.x;
-            bk[i] = gk.y;
-            sv[i] = gv.x;
-            bv[i] = gv.y;
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int t = 0; t < NCT; ++t) {
+                    x.s[u][t][0] *= own[t];
+                    x.s[u][t][1] *= own[t];
+                }
         }
-        f32x4 s[NCT][2];
 #pragma unroll
-        for (int t = 0; t < NCT; ++t) s[t][0] = s[t][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int u = 0; u < SUB; ++u) {
+            float sk[8], bk[8];                           // of tokens 8 g + i
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+            for (int i = 0; i < 8; ++i) {
+                const float2 gk = mem(u)[8u * g + i];
+                sk[i] = gk.x;
+                bk[i] = gk.y;
+                sv_top = fmaxf(sv_top, mem(u)[32u + 8u * g + i].x);
+            }
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const f16x8 a = key(j, k);
+            for (int t = 0; t < NCT; ++t)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x.s[u][t][i / 4][i % 4] = fmaf(x.s[u][t][i / 4][i % 4], sk[i], fmaf(bk[i], bq[t], -m[t]));
+        }
+        if (!whole) {
+            uint32_t from = t0 + 8u * g;
+#if defined(__AMDGCN__)
+            asm volatile("" : "+v"(from));   // (keeps this inside the branch: else it is in every step)
+#endif
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
 #pragma unroll
                 for (int t = 0; t < NCT; ++t)
 #pragma unroll
-                    for (int z = PIECES - 1; z >= 0; --z) s[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, q[t][z][k], s[t][j], 0, 0, 0);
-            }
-        float y[NCT][8], top[NCT];
-        float sv_top = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sv_top = fmaxf(sv_top, sv[i]);
+                    for (int i = 0; i < 8; ++i) {
+                        const int32_t tok = (int32_t)from + 32 * u + i;
+                        if (!there(u) || tok < lo[t] || tok >= hi[t]) x.s[u][t][i / 4][i % 4] = -INFINITY;
+                    }
+        }
         bool moves = sv_top > sv_most;
 #pragma unroll
         for (int t = 0; t < NCT; ++t) {
+            top[t] = x.s[0][t][0][0];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[t][i] = fmaf(s[t][i / 4][i % 4], sk[i], bk[i] * bq[t]);
-            if (!whole) {
-                uint32_t from = t0 + 8u * g;
-#if defined(__AMDGCN__)
-                asm volatile("" : "+v"(from));   // (keeps this inside the branch: else 24 instructions of it are in every step)
-#endif
+            for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int32_t tok = (int32_t)from + i;
-                    if (!there || tok < lo[t] || tok >= hi[t]) y[t][i] = -INFINITY;
-                }
-            }
-            top[t] = y[t][0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) top[t] = fmaxf(top[t], y[t][i]);
-            moves |= (top[t] - m[t]) * f[t] > kAtHeadroom;
+                for (int i = u ? 0 : 1; i < 8; ++i) top[t] = fmaxf(top[t], x.s[u][t][i / 4][i % 4]);
+            moves |= top[t] > over[t];
         }
-        if (__ballot(moves) != 0ull) rescale(top, sv_top);
-        f16x8 p[NCT][PIECES];
+        if (__ballot(moves) != 0ull) rescale<SUB>(x.s, top, sv_top);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sv[i] *= norm;
-#pragma unroll
-        for (int t = 0; t < NCT; ++t) {
-            const float mf = -m[t] * f[t];
+        for (int u = 0; u < SUB; ++u) {
+            f16x8 p[NCT][PIECES];
+            float sv[8], bv[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float e = at_exp2(fmaf(y[t][i], f[t], mf));
-                l[t] += e;
-                lv[t] = fmaf(e, bv[i], lv[t]);
-                const float w = e * sv[i];
-                const int at = i % 4 * 2 + i / 4;         // code order
-                p[t][0][at] = (_Float16)w;
-                if constexpr (PIECES == 2) p[t][1][at] = (_Float16)(w - (float)p[t][0][at]);
+                const float2 gv = mem(u)[32u + 8u * g + i];
+                sv[i] = gv.x * norm;
+                bv[i] = gv.y;
             }
-        }
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const f16x8 a = value(b);
+            for (int t = 0; t < NCT; ++t) {
 #pragma unroll
-            for (int t = 0; t < NCT; ++t)
-                if constexpr (PIECES == 1) {
-                    o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][0], o[t][b], 0, 0, 0);
-                } else {
-                    // added up outside the matrix unit: its sums of the whole row drift by a few 2^-18 (measured 3e-6 of the answer at
-                    // 1000 tokens; so 7e-7, the plain fp32 form's error)
-                    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-                    const f32x4 part = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][1], zero, 0, 0, 0);
-                    o[t][b] += __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][0], part, 0, 0, 0);
+                for (int i = 0; i < 8; ++i) {
+                    const float e = at_exp2(x.s[u][t][i / 4][i % 4]);
+                    l[t] += e;
+                    lv[t] = fmaf(e, bv[i], lv[t]);
+                    const float w = e * sv[i];
+                    const int at = i % 4 * 2 + i / 4;     // code order
+                    p[t][0][at] = (_Float16)w;
+                    if constexpr (PIECES == 2) p[t][1][at] = (_Float16)(w - (float)p[t][0][at]);
                 }
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const f16x8 a = value(u, b);
+#pragma unroll
+                for (int t = 0; t < NCT; ++t)
+                    if constexpr (PIECES == 1) {
+                        o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][0], o[t][b], 0, 0, 0);
+                    } else {
+                        // added up outside the matrix unit: its sums of the whole row drift by a few 2^-18 (measured 3e-6 of the answer at
+                        // 1000 tokens; so 7e-7, the plain fp32 form's error)
+                        const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+                        const f32x4 part = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][1], zero, 0, 0, 0);
+                        o[t][b] += __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][0], part, 0, 0, 0);
+                    }
+            }
         }
     }
 
     // One wave for itself: 32 tokens that it has loaded.  `mem`: this wave's own.
-    __device__ __forceinline__ void step_alone(const Raw &x, float2 *mem, const AtMagic &magic, uint32_t t0, bool whole, bool there)
+    __device__ __forceinline__ void step_alone(const Raw &x, float2 *mem, const AtMagic &magic, float key_factor, uint32_t t0, bool whole, bool there)
     {
-        mem[threadIdx.x % kWave] = centred(x.grid, x.written);
+        mem[threadIdx.x % kWave] = centred(x.grid, x.written, key_factor);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        step([&](int j, int k) { return at_codes(x.k[j][k], magic); }, [&](int b) { return at_codes(x.v[b], magic); }, mem, t0, whole, there);
+        Scores<1> s;
+        products<1>(s, [&](int, int j, int k) { return at_codes(x.k[j][k], magic); });
+        weigh<1>(s, [&](int, int b) { return at_codes(x.v[b], magic); }, [&](int) { return mem; }, t0, whole, [&](int) { return there; });
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
@@ -534,7 +585,7 @@ template <int D, int NCT, int DT> struct AtWave {
             l[t] += kv_xor_f32(l[t], 32);
             lv[t] += kv_xor_f32(lv[t], 16);
             lv[t] += kv_xor_f32(lv[t], 32);
-            m[t] = l[t] == 0.0f ? -3.402823466e38f : m[t] * f[t];   // (a column that saw nothing: below any other)
+            m[t] = l[t] == 0.0f ? -3.402823466e38f : m[t];   // (a column that saw nothing: below any other)
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -687,13 +738,14 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 ? QP_KV_FEW_WAVES : 1) void k_
     int32_t sees_lo, sees_hi;
     at_sees<Wave, 1>(x, sees_lo, sees_hi);
     const AtMagic magic;
+    const float key_factor = a.scale * (1.44269504088896341f / 16.0f);
     for (; t0 < b.t1; t0 += kAtTile) {
         if (t0 + kAtTile < b.t1) {
             const unsigned char *slab = slab_at(t0 + kAtTile, there_next);
             x.load(nxt, slab, t0 + kAtTile, c.page_shift, b.row.length, there_next);
         }
         const bool whole = there && (int32_t)t0 >= sees_lo && (int32_t)(t0 + kAtStep) <= sees_hi;
-        x.step_alone(cur, grids[wave], magic, t0, whole, there);
+        x.step_alone(cur, grids[wave], magic, key_factor, t0, whole, there);
         cur = nxt;
         there = there_next;
     }
@@ -743,6 +795,7 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? QP_KV_MANY_
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u;
     const uint32_t col0 = min(b.p.col0 + wave * 16u * NCT, b.p.col1), col1 = min(col0 + 16u * NCT, b.p.col1);
     const AtMagic magic;
+    const float key_factor = a.scale * (1.44269504088896341f / 16.0f);
     // Every wave takes a quarter of a stage's words apart for all of them: while the waves go through a stage, the next one's
     // fragments go to the other half of LDS and the words of the one after it are on their way.  A wave has one of the two tiles of
     // keys and half of the values of 32 tokens, each one load (of heads of 256 either a tile of keys or half of the values: the stage
@@ -773,7 +826,7 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? QP_KV_MANY_
         const unsigned char *slab = kv_slab(c, page < 0 ? 0 : page, b.p.head), *codes = slab + (size_t)in * (D / 2);
         if (keys) __builtin_memcpy(wk, codes + key_at, sizeof wk);
         if (values) __builtin_memcpy(wv, codes + value_at, sizeof wv);   // (an odd number of blocks: the last word is not this head's, and not used)
-        if (side == 0u && keys) grid = *reinterpret_cast<const float2 *>(slab + (size_t)in * 8u + grid_at);
+        if (keys) grid = *reinterpret_cast<const float2 *>(slab + (size_t)in * 8u + grid_at);
         written = page >= 0 && (int32_t)(at + lane % 32u) < b.row.length;
     };
     const auto put = [&](uint32_t half) {
@@ -787,34 +840,35 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? QP_KV_MANY_
             for (uint32_t i = 0; i < (uint32_t)kHalf; ++i)
                 if (NB % 2 == 0 || side * kHalf + i < (uint32_t)NB) st.frags[2 * KS + side * kHalf + i][lane] = at_codes(wv[i], magic);
         }
-        if (side == 0u && keys) st.grids[lane] = Wave::centred(grid, written);
+        if (keys) st.grids[lane] = Wave::centred(grid, written, key_factor);      // (both sides the same: no branch)
     };
     uint32_t half = 0u;
-    if (b.t0 < b.t1) fetch(b.t0, there[0]);                         // (on their way while the queries are made ready)
+    fetch(b.t0, there[0]);                                          // (on its way while the queries are made ready; past the end: page 0, unused)
     Wave x;
     x.load_query(c, qv, a, b.row, b.p.head, col0, col1);
     int32_t sees_lo, sees_hi;
     at_sees<Wave, NCT>(x, sees_lo, sees_hi);
     uint32_t w_lo = 0u, w_hi = 0u;                                  // what any of this wave's columns sees
     if (col0 < col1) at_range(b.row, a, col0, col1, w_lo, w_hi);
-    if (b.t0 < b.t1) {
-        put(0u);
-        if (b.t0 + kStage < b.t1) fetch(b.t0 + kStage, there[1]);
-    }
+    put(0u);
+    fetch(b.t0 + kStage, there[1]);
     __syncthreads();
     for (uint32_t t = b.t0; t < b.t1; t += kStage) {
-        if (t + kStage < b.t1) {
-            put(half ^ 1u);
-            if (t + 2u * kStage < b.t1) fetch(t + 2u * kStage, there[2]);
-        }
+        if (t + kStage > w_lo && t < w_hi) {
+            const Stage(&st)[kSub] = stages[half];
+            bool all = true;
 #pragma unroll
-        for (uint32_t u = 0; u < kSub; ++u) {
-            const uint32_t at = t + u * kAtStep;
-            if (at + kAtStep > w_lo && at < min(w_hi, b.t1)) {
-                const Stage &st = stages[half][u];
-                const bool whole = there[0][u] && (int32_t)at >= sees_lo && (int32_t)(at + kAtStep) <= sees_hi;
-                x.step([&](int j, int k) { return st.frags[j * KS + k][lane]; }, [&](int i) { return st.frags[2 * KS + i][lane]; }, st.grids, at, whole, there[0][u]);
-            }
+            for (uint32_t u = 0; u < kSub; ++u) all = all && there[0][u];
+            const bool whole = all && (int32_t)t >= sees_lo && (int32_t)(t + kStage) <= sees_hi;
+            typename Wave::template Scores<kSub> s;
+            x.template products<kSub>(s, [&](int u, int j, int k) { return st[u].frags[j * KS + k][lane]; });
+            put(half ^ 1u);                   // (between the products, as far as the compiler mixes them: the one is the matrix unit's)
+            fetch(t + 2u * kStage, there[2]);
+            x.template weigh<kSub>(s, [&](int u, int i) { return st[u].frags[2 * KS + i][lane]; }, [&](int u) { return st[u].grids; }, t, whole,
+                                   [&](int u) { return there[0][u]; });
+        } else {
+            put(half ^ 1u);
+            fetch(t + 2u * kStage, there[2]);
         }
         __syncthreads();
         half ^= 1u;
