@@ -117,12 +117,13 @@ inline size_t at_bytes(const KvLayer &c, uint32_t dim, uint32_t group, size_t &f
 
 // ---- which piece of which item a block has ---------------------------------------------------------------------------------
 struct AtRow {
+    KvRow row;
     uint32_t items, first, cols, tiles;          // items from column `first` on; `cols`: where the last one ends
 };
 template <bool MANY> __device__ __forceinline__ AtRow at_row(const KvLayer &c, const KvAttn &a, bool wide, uint32_t r)
 {
-    const KvRow row = kv_row(c, r);
     AtRow o;
+    const KvRow row = o.row = kv_row(c, r);
     const uint32_t cols = (uint32_t)row.count * a.group, rest = cols % kAtCols<true>;
     const bool small = rest <= kAtUnit;          // the rest is for `few`
     o.first = !MANY && wide ? (small ? cols - rest : cols) : 0u;
@@ -134,6 +135,7 @@ template <bool MANY> __device__ __forceinline__ AtRow at_row(const KvLayer &c, c
     return o;
 }
 struct AtPiece {
+    KvRow at;
     uint32_t row, head, col0, col1, s, pieces;   // columns; pieces: at most so many of the item's tokens
     uint32_t per;                                // tiles that a piece should have
     uint32_t unit, rec;                          // where the item's partial results and its columns' records go
@@ -170,56 +172,107 @@ __device__ __forceinline__ uint64_t at_wave_sum(uint64_t v)
     return v;
 }
 
+// What a row adds to the call: blocks, units of partial results, columns with records.
+template <bool MANY> struct AtParts {
+    uint32_t pieces, blocks, units, cols;
+    __device__ __forceinline__ AtParts(const KvLayer &c, const AtRow &o, uint32_t per)
+    {
+        pieces = (o.tiles + per - 1u) / per;
+        blocks = c.kv_heads * o.items * pieces;
+        units = pieces > 1u ? blocks * (kAtCols<MANY> / kAtUnit) : 0u;
+        cols = pieces > 1u ? c.kv_heads * (o.cols - o.first) : 0u;
+    }
+    // `e`: where its parts end among all rows'.  True where the rows' tokens do not overlap: what the host sized the grid and the workspace for.
+    __device__ __forceinline__ bool fits(const AtWork &w, const uint32_t (&e)[3]) const
+    {
+        return e[0] - blocks <= gridDim.x && e[0] <= gridDim.x && e[1] - units <= w.most_units && e[1] <= w.most_units && e[2] - cols <= w.most_cols &&
+               e[2] <= w.most_cols;
+    }
+    // the row's block i
+    __device__ __forceinline__ AtPiece piece(const KvLayer &c, const AtRow &o, uint32_t r, uint32_t per, const uint32_t (&e)[3], uint32_t i) const
+    {
+        AtPiece f;
+        f.at = o.row;
+        f.row = r;
+        f.head = i % c.kv_heads;                 // heads side by side: an XCD per head, whose tokens its L2 then holds
+        i /= c.kv_heads;
+        f.s = i % pieces;
+        const uint32_t item = o.items - 1u - i / pieces;          // the last columns, which see the most tokens, first
+        f.col0 = o.first + item * kAtCols<MANY>;
+        f.col1 = min(f.col0 + kAtCols<MANY>, o.cols);
+        f.pieces = pieces;
+        f.per = per;
+        f.unit = e[1] - units + (item * c.kv_heads + f.head) * pieces * (kAtCols<MANY> / kAtUnit);
+        f.rec = e[2] - cols + (f.col0 - o.first) * c.kv_heads + f.head * (f.col1 - f.col0);
+        return f;
+    }
+};
+template <bool MANY> __device__ __forceinline__ uint32_t at_share(const KvLayer &c, uint64_t cost)
+{
+    return (uint32_t)min(max((cost * c.kv_heads + kAtTarget<MANY> - 1u) / kAtTarget<MANY>, (uint64_t)kAtLeast), (uint64_t)0x7fffffffu);
+}
+
 // False: the call has fewer pieces than blocks.
 template <bool MANY> __device__ __forceinline__ bool at_find(const KvLayer &c, const KvAttn &a, const AtWork &w, uint32_t block, AtPiece &mine)
 {
-    constexpr uint32_t kUnits = kAtCols<MANY> / kAtUnit;
+    const uint32_t tid = threadIdx.x, lane = tid % kWave;
+    const AtRow none{KvRow{0, 0, 0}, 0u, 0u, 0u, 1u};
+    if (c.rows <= (uint32_t)kWave) {             // every wave for itself, a row a lane: nothing to wait for but the lengths
+        const AtRow o = lane < c.rows ? at_row<MANY>(c, a, w.wide, lane) : none;
+        const uint32_t per = at_share<MANY>(c, at_wave_sum((uint64_t)o.tiles * o.items));
+        const AtParts<MANY> parts(c, o, per);
+        uint32_t e[3] = {parts.blocks, parts.units, parts.cols};
+#pragma unroll
+        for (uint32_t d = 1; d < (uint32_t)kWave; d *= 2u)
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                const uint32_t x = __shfl_up(e[i], d, kWave);
+                if (lane >= d) e[i] += x;
+            }
+        const bool fits = parts.fits(w, e);
+        if (block == 0u && tid < (uint32_t)kWave) {
+            const uint32_t split = wave_max_u32(fits && parts.cols != 0u ? e[2] : 0u);
+            if (tid == 0u) w.header[0] = split;
+        }
+        const uint64_t owner = __ballot(fits && block >= e[0] - parts.blocks && block < e[0]);
+        if (owner == 0ull) return false;
+        const int from = __builtin_ctzll(owner);
+        const auto get = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, from); };
+        AtRow row{KvRow{(int32_t)get((uint32_t)o.row.begin), (int32_t)get((uint32_t)o.row.count), (int32_t)get((uint32_t)o.row.length)},
+                  get(o.items), get(o.first), get(o.cols), get(o.tiles)};
+        const uint32_t end[3] = {get(e[0]), get(e[1]), get(e[2])};
+        const AtParts<MANY> its(c, row, per);
+        mine = its.piece(c, row, (uint32_t)from, per, end, block - (end[0] - its.blocks));
+        return true;
+    }
     __shared__ uint32_t part[kAtWaves][3];
     __shared__ uint64_t work[kAtWaves];
     __shared__ AtPiece found;
     __shared__ uint32_t have, split;
-    const uint32_t tid = threadIdx.x;
-    const AtRow none{0u, 0u, 0u, 1u};
-    const AtRow mine0 = tid < c.rows ? at_row<MANY>(c, a, w.wide, tid) : none;      // (most calls have no more rows than that)
-    uint64_t cost = (uint64_t)mine0.tiles * mine0.items;
+    const AtRow mine0 = at_row<MANY>(c, a, w.wide, min(tid, c.rows - 1u));          // (most calls have no more rows than that)
+    uint64_t cost = tid < c.rows ? (uint64_t)mine0.tiles * mine0.items : 0u;
     for (uint32_t r = tid + kAtThreads; r < c.rows; r += kAtThreads) {
         const AtRow o = at_row<MANY>(c, a, w.wide, r);
         cost += (uint64_t)o.tiles * o.items;
     }
     cost = at_wave_sum(cost);
-    if (tid % kWave == 0u) work[tid / kWave] = cost;
+    if (lane == 0u) work[tid / kWave] = cost;
     if (tid == 0u) have = split = 0u;
     __syncthreads();
-    const uint64_t all = (work[0] + work[1] + work[2] + work[3]) * c.kv_heads;
-    const uint32_t per = (uint32_t)min(max((all + kAtTarget<MANY> - 1u) / kAtTarget<MANY>, (uint64_t)kAtLeast), (uint64_t)0x7fffffffu);
+    const uint32_t per = at_share<MANY>(c, work[0] + work[1] + work[2] + work[3]);
     uint32_t before[3] = {0u, 0u, 0u};                   // blocks, units, columns of the rows so far
     for (uint32_t r0 = 0; r0 < c.rows; r0 += kAtThreads) {
         const uint32_t r = r0 + tid;
-        const AtRow o = r0 == 0u ? mine0 : r < c.rows ? at_row<MANY>(c, a, w.wide, r) : none;
-        const uint32_t pieces = (o.tiles + per - 1u) / per, blocks = c.kv_heads * o.items * pieces;
-        const uint32_t units = pieces > 1u ? blocks * kUnits : 0u, cols = pieces > 1u ? c.kv_heads * (o.cols - o.first) : 0u;
-        uint32_t x[3] = {blocks, units, cols}, total[3];
-        at_scan(x, part, total);
-        const uint32_t eb = before[0] + x[0], eu = before[1] + x[1], ek = before[2] + x[2];      // ends
-        const uint32_t pb = eb - blocks, pu = eu - units, pk = ek - cols;
-        // (always so where the rows' tokens do not overlap: what the host sized the grid and the workspace for)
-        const bool fits = pb <= gridDim.x && eb <= gridDim.x && pu <= w.most_units && eu <= w.most_units && pk <= w.most_cols && ek <= w.most_cols;
-        if (fits && cols != 0u) atomicMax(&split, ek);
-        if (fits && block >= pb && block < eb) {
-            uint32_t i = block - pb;                     // heads side by side: an XCD per head, whose tokens its L2 then holds
-            AtPiece f;
-            f.row = r;
-            f.head = i % c.kv_heads;
-            i /= c.kv_heads;
-            f.s = i % pieces;
-            const uint32_t item = o.items - 1u - i / pieces;       // the last columns, which see the most tokens, first
-            f.col0 = o.first + item * kAtCols<MANY>;
-            f.col1 = min(f.col0 + kAtCols<MANY>, o.cols);
-            f.pieces = pieces;
-            f.per = per;
-            f.unit = pu + (item * c.kv_heads + f.head) * pieces * kUnits;
-            f.rec = pk + (f.col0 - o.first) * c.kv_heads + f.head * (f.col1 - f.col0);
-            found = f;
+        const AtRow o = r >= c.rows ? none : r0 == 0u ? mine0 : at_row<MANY>(c, a, w.wide, r);
+        const AtParts<MANY> parts(c, o, per);
+        uint32_t e[3] = {parts.blocks, parts.units, parts.cols}, total[3];
+        at_scan(e, part, total);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) e[k] += before[k];
+        const bool fits = parts.fits(w, e);
+        if (fits && parts.cols != 0u) atomicMax(&split, e[2]);
+        if (fits && block >= e[0] - parts.blocks && block < e[0]) {
+            found = parts.piece(c, o, r, per, e, block - (e[0] - parts.blocks));
             have = 1u;
         }
 #pragma unroll
@@ -261,6 +314,15 @@ struct AtMagic {
 #endif
     }
 };
+// A word that was loaded steps ago, looked at only now.  (Left to itself the compiler moves the first instructions of at_codes up to the
+// load and waits for it there: attend_prompt 367 -> 387 us.)
+__device__ __forceinline__ uint32_t at_now(uint32_t w)
+{
+#if defined(__AMDGCN__)
+    asm volatile("" : "+v"(w));
+#endif
+    return w;
+}
 __device__ __forceinline__ f16x8 at_codes(uint32_t w, const AtMagic &k)
 {
     const f16x2 big = {(_Float16)-1032.0f, (_Float16)-1032.0f}, small = {(_Float16)-72.0f, (_Float16)-72.0f};
@@ -293,82 +355,84 @@ template <int D, int NCT, int DT> struct AtWave {
         bool written;                                // else the grid may be anything (looked at when it is used: not to wait for it before)
     };
 
-    __device__ __forceinline__ void load_query(const KvLayer &c, const KvView &qv, const KvAttn &a, const KvRow &row, uint32_t head,
-                                               uint32_t col0, uint32_t cols)
+    // A lane's elements of a column tile's queries as they lie in memory: 8 KS of a column's, from 8 g KS on.
+    struct Query {
+        u32x4 w[KS][DT == QP_F32 ? 2 : 1];
+    };
+    __device__ __forceinline__ void load_query(Query &x, const KvView &qv, const KvAttn &a, const KvRow &row, uint32_t head, int t, uint32_t col0, uint32_t cols) const
     {
-        const uint32_t lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u;
+        const uint32_t lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u, col = col0 + 16u * t + n;
+        const bool is = col < cols;
+        const uint32_t i = is ? col / a.group : 0u, h = head * a.group + (is ? col % a.group : 0u);
+        const unsigned char *src = qv.data + ((uint64_t)row.begin + i) * qv.token_stride + (uint64_t)h * qv.head_stride;
 #pragma unroll
-        for (int t = 0; t < NCT; ++t) {
-            const uint32_t col = col0 + 16u * t + n;
-            const bool is = col < cols;
-            const uint32_t i = is ? col / a.group : 0u, h = head * a.group + (is ? col % a.group : 0u);
-            const unsigned char *src = qv.data + ((uint64_t)row.begin + i) * qv.token_stride + (uint64_t)h * qv.head_stride;
-            float x[KS][8];
-            float top = 0.0f;
-            bool bad = false;
+        for (int s = 0; s < KS; ++s) {
+            const uint32_t unit = g * KS + s;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const uint32_t unit = g * KS + s;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[s][e] = 0.0f;
-                if (is && unit * 8u < (uint32_t)D) {
-                    if constexpr (DT == QP_F32) {
-                        const f32x4 u = reinterpret_cast<const f32x4 *>(src)[2u * unit], v = reinterpret_cast<const f32x4 *>(src)[2u * unit + 1u];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            x[s][e] = u[e];
-                            x[s][4 + e] = v[e];
-                        }
-                    } else {
-                        Vec16<DT>::load(src, unit, x[s]);
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    bad |= (__float_as_uint(x[s][e]) & 0x7f800000u) == 0x7f800000u;
-                    top = fmaxf(top, fabsf(x[s][e]));
-                }
+            for (int z = 0; z < (DT == QP_F32 ? 2 : 1); ++z) {
+                x.w[s][z] = u32x4{0u, 0u, 0u, 0u};
+                if (is && unit * 8u < (uint32_t)D) x.w[s][z] = reinterpret_cast<const u32x4 *>(src)[unit * (DT == QP_F32 ? 2u : 1u) + z];
             }
-            top = fmaxf(top, kv_xor_f32(top, 16));
-            top = fmaxf(top, kv_xor_f32(top, 32));
-            uint32_t any = bad ? 1u : 0u;
-            any |= __shfl_xor(any, 16, kWave);
-            any |= __shfl_xor(any, 32, kWave);
-            int32_t up = 4;
-            if (top != 0.0f && any == 0u && !(top >= 0x1p-4f && top < 0x1p11f)) {
-                int32_t ex;
-                (void)frexpf(top, &ex);
-                up = min(15 - ex, 100);                  // q 2^up: the largest element in [2^14, 2^15)
-            }
-            own[t] = ldexpf(1.0f, 4 - up);
-            owns = (t != 0 && owns) || __ballot(up != 4) != 0ull;
-            float sum = 0.0f;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                f16x8 high, low;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {            // code order 0, 4, 1, 5, 2, 6, 3, 7
-                    const int src_e = e % 2 * 4 + e / 2;
-                    const float y = any ? 0.0f : ldexpf(x[s][src_e], up);
-                    sum += y;
-                    high[e] = (_Float16)y;
-                    low[e] = (_Float16)(y - (float)high[e]);
-                }
-                q[t][0][s] = high;
-                if constexpr (PIECES == 2) q[t][1][s] = low;
-            }
-            sum += kv_xor_f32(sum, 16);
-            sum += kv_xor_f32(sum, 32);
-            bq[t] = any ? __uint_as_float(0x7fc00000u) : sum * own[t];
-            m[t] = 0.0f;
-            over[t] = -INFINITY;
-            l[t] = lv[t] = 0.0f;
-#pragma unroll
-            for (int b = 0; b < NB; ++b) o[t][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            const int64_t pos = (int64_t)row.length - row.count + i;
-            hi[t] = !is ? 0x7fffffff : a.causal ? (int32_t)max((int64_t)0, min(pos + 1, (int64_t)row.length)) : row.length;
-            lo[t] = is && a.window ? (int32_t)max((int64_t)0, pos - (int64_t)a.window + 1) : 0;
         }
+    }
+    // Column tile t's fragments, and its columns' state.
+    __device__ __forceinline__ void make_query(const Query &w, const KvAttn &a, const KvRow &row, int t, uint32_t col0, uint32_t cols)
+    {
+        const uint32_t col = col0 + 16u * t + threadIdx.x % 16u;
+        const bool is = col < cols;
+        const uint32_t i = is ? col / a.group : 0u;
+        float x[KS][8];
+        float top = 0.0f;
+        bool bad = false;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (DT == QP_F32) x[s][e] = __uint_as_float(w.w[s][e / 4][e % 4]);
+                else x[s][e] = __uint_as_float(e % 2 ? w.w[s][0][e / 2] & 0xffff0000u : w.w[s][0][e / 2] << 16);
+                bad |= (__float_as_uint(x[s][e]) & 0x7f800000u) == 0x7f800000u;
+                top = fmaxf(top, fabsf(x[s][e]));
+            }
+        }
+        top = fmaxf(top, kv_xor_f32(top, 16));
+        top = fmaxf(top, kv_xor_f32(top, 32));
+        uint32_t any = bad ? 1u : 0u;
+        any |= __shfl_xor(any, 16, kWave);
+        any |= __shfl_xor(any, 32, kWave);
+        int32_t up = 4;
+        if (top != 0.0f && any == 0u && !(top >= 0x1p-4f && top < 0x1p11f)) {
+            int32_t ex;
+            (void)frexpf(top, &ex);
+            up = min(15 - ex, 100);                  // q 2^up: the largest element in [2^14, 2^15)
+        }
+        own[t] = ldexpf(1.0f, 4 - up);
+        owns = (t != 0 && owns) || __ballot(up != 4) != 0ull;
+        float sum = 0.0f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            f16x8 high, low;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {            // code order 0, 4, 1, 5, 2, 6, 3, 7
+                const int src_e = e % 2 * 4 + e / 2;
+                const float y = any ? 0.0f : ldexpf(x[s][src_e], up);
+                sum += y;
+                high[e] = (_Float16)y;
+                low[e] = (_Float16)(y - (float)high[e]);
+            }
+            q[t][0][s] = high;
+            if constexpr (PIECES == 2) q[t][1][s] = low;
+        }
+        sum += kv_xor_f32(sum, 16);
+        sum += kv_xor_f32(sum, 32);
+        bq[t] = any ? __uint_as_float(0x7fc00000u) : sum * own[t];
+        m[t] = 0.0f;
+        over[t] = -INFINITY;
+        l[t] = lv[t] = 0.0f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) o[t][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        const int64_t pos = (int64_t)row.length - row.count + i;
+        hi[t] = !is ? 0x7fffffff : a.causal ? (int32_t)max((int64_t)0, min(pos + 1, (int64_t)row.length)) : row.length;
+        lo[t] = is && a.window ? (int32_t)max((int64_t)0, pos - (int64_t)a.window + 1) : 0;
         norm = 1.0f;
         norm_exp = 0;
         sv_most = 0.0f;
@@ -569,8 +633,8 @@ template <int D, int NCT, int DT> struct AtWave {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         Scores<1> s;
-        products<1>(s, [&](int, int j, int k) { return at_codes(x.k[j][k], magic); });
-        weigh<1>(s, [&](int, int b) { return at_codes(x.v[b], magic); }, [&](int) { return mem; }, t0, whole, [&](int) { return there; });
+        products<1>(s, [&](int, int j, int k) { return at_codes(at_now(x.k[j][k]), magic); });
+        weigh<1>(s, [&](int, int b) { return at_codes(at_now(x.v[b]), magic); }, [&](int) { return mem; }, t0, whole, [&](int) { return there; });
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
@@ -624,7 +688,10 @@ template <bool MANY> __device__ __forceinline__ bool at_begin(const KvLayer &c, 
     p.head = __builtin_amdgcn_readfirstlane(p.head);
     p.col0 = __builtin_amdgcn_readfirstlane(p.col0);
     p.col1 = __builtin_amdgcn_readfirstlane(p.col1);
-    b.row = kv_row(c, p.row);
+    p.s = __builtin_amdgcn_readfirstlane(p.s);
+    p.pieces = __builtin_amdgcn_readfirstlane(p.pieces);
+    p.per = __builtin_amdgcn_readfirstlane(p.per);
+    b.row = KvRow{__builtin_amdgcn_readfirstlane(p.at.begin), __builtin_amdgcn_readfirstlane(p.at.count), __builtin_amdgcn_readfirstlane(p.at.length)};
     uint32_t lo, hi;
     at_range(b.row, a, p.col0, p.col1, lo, hi);
     const uint32_t first = lo / kAtTile, tiles = hi > lo ? (hi + kAtTile - 1u) / kAtTile - first : 0u;
@@ -635,8 +702,10 @@ template <bool MANY> __device__ __forceinline__ bool at_begin(const KvLayer &c, 
             w.cols[p.rec + k] = u32x4{p.unit * kAtUnit + k, b.pieces > 1u ? b.pieces : 0u, kAtCols<MANY>, place * (c.kv_heads * a.group) + h};
         }
     if (p.s >= b.pieces) return false;
-    b.t0 = (first + (uint32_t)((uint64_t)tiles * p.s / b.pieces)) * kAtTile;
-    b.t1 = min((first + (uint32_t)((uint64_t)tiles * (p.s + 1u) / b.pieces)) * kAtTile, hi);
+    const uint32_t each = tiles / b.pieces, more = tiles % b.pieces;          // (the first `more` pieces have one more)
+    const uint32_t from = first + p.s * each + min(p.s, more);
+    b.t0 = from * kAtTile;
+    b.t1 = min((from + each + (p.s < more ? 1u : 0u)) * kAtTile, hi);
     return true;
 }
 // The tokens that all of a wave's columns see.
@@ -700,6 +769,9 @@ __device__ __forceinline__ void at_store(const AtWave<D, NCT, DT> &x, const AtBl
 #ifndef QP_KV_FEW_WAVES
 #define QP_KV_FEW_WAVES 2
 #endif
+#ifndef QP_AHEAD
+#define QP_AHEAD 2
+#endif
 #ifndef QP_SUB
 #define QP_SUB 2
 #endif
@@ -724,30 +796,41 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 ? QP_KV_FEW_WAVES : 1) void k_
         there = page >= 0;
         return kv_slab(c, there ? page : 0, b.p.head);
     };
+    // Three steps' words: those of a step are fetched again, for the one after the next two, as soon as it is done with them.
+    constexpr int kAhead = QP_AHEAD;
     Wave x;
-    typename Wave::Raw cur, nxt;
-    bool there = false, there_next = false;
+    typename Wave::Query query;
+    typename Wave::Raw raw[kAhead];
+    bool there[kAhead];
     uint32_t t0 = b.t0 + wave * kAtStep;
     x.place(c.page_shift);
+    x.load_query(query, qv, a, b.row, b.p.head, 0, b.p.col0, b.p.col1);       // (all of it on its way at once)
     pages.load(c, b.p.row, t0 >> c.page_shift);
-    if (t0 < b.t1) {                          // (on its way while the queries are made ready)
-        const unsigned char *slab = slab_at(t0, there);
-        x.load(cur, slab, t0, c.page_shift, b.row.length, there);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        there[i] = false;
+        if (t0 + i * kAtTile < b.t1) {
+            const unsigned char *slab = slab_at(t0 + i * kAtTile, there[i]);
+            x.load(raw[i], slab, t0 + i * kAtTile, c.page_shift, b.row.length, there[i]);
+        }
     }
-    x.load_query(c, qv, a, b.row, b.p.head, b.p.col0, b.p.col1);
+    x.make_query(query, a, b.row, 0, b.p.col0, b.p.col1);
     int32_t sees_lo, sees_hi;
     at_sees<Wave, 1>(x, sees_lo, sees_hi);
     const AtMagic magic;
     const float key_factor = a.scale * (1.44269504088896341f / 16.0f);
-    for (; t0 < b.t1; t0 += kAtTile) {
-        if (t0 + kAtTile < b.t1) {
-            const unsigned char *slab = slab_at(t0 + kAtTile, there_next);
-            x.load(nxt, slab, t0 + kAtTile, c.page_shift, b.row.length, there_next);
+    while (t0 < b.t1) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (t0 >= b.t1) break;
+            const bool whole = there[i] && (int32_t)t0 >= sees_lo && (int32_t)(t0 + kAtStep) <= sees_hi;
+            x.step_alone(raw[i], grids[wave], magic, key_factor, t0, whole, there[i]);
+            if (t0 + kAhead * kAtTile < b.t1) {
+                const unsigned char *slab = slab_at(t0 + kAhead * kAtTile, there[i]);
+                x.load(raw[i], slab, t0 + kAhead * kAtTile, c.page_shift, b.row.length, there[i]);
+            }
+            t0 += kAtTile;
         }
-        const bool whole = there && (int32_t)t0 >= sees_lo && (int32_t)(t0 + kAtStep) <= sees_hi;
-        x.step_alone(cur, grids[wave], magic, key_factor, t0, whole, there);
-        cur = nxt;
-        there = there_next;
     }
     x.finish();
 #pragma unroll
@@ -833,19 +916,24 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? QP_KV_MANY_
         Stage &st = stages[half][mine];
         if (keys) {
 #pragma unroll
-            for (uint32_t k = 0; k < (uint32_t)KS; ++k) st.frags[side * KS + k][lane] = at_codes(wk[k], magic);
+            for (uint32_t k = 0; k < (uint32_t)KS; ++k) st.frags[side * KS + k][lane] = at_codes(at_now(wk[k]), magic);
         }
         if (values) {
 #pragma unroll
             for (uint32_t i = 0; i < (uint32_t)kHalf; ++i)
-                if (NB % 2 == 0 || side * kHalf + i < (uint32_t)NB) st.frags[2 * KS + side * kHalf + i][lane] = at_codes(wv[i], magic);
+                if (NB % 2 == 0 || side * kHalf + i < (uint32_t)NB) st.frags[2 * KS + side * kHalf + i][lane] = at_codes(at_now(wv[i]), magic);
         }
         if (keys) st.grids[lane] = Wave::centred(grid, written, key_factor);      // (both sides the same: no branch)
     };
     uint32_t half = 0u;
     fetch(b.t0, there[0]);                                          // (on its way while the queries are made ready; past the end: page 0, unused)
     Wave x;
-    x.load_query(c, qv, a, b.row, b.p.head, col0, col1);
+    typename Wave::Query query;
+#pragma unroll
+    for (int i = 0; i < NCT; ++i) {
+        x.load_query(query, qv, a, b.row, b.p.head, i, col0, col1);
+        x.make_query(query, a, b.row, i, col0, col1);
+    }
     int32_t sees_lo, sees_hi;
     at_sees<Wave, NCT>(x, sees_lo, sees_hi);
     uint32_t w_lo = 0u, w_hi = 0u;                                  // what any of this wave's columns sees

@@ -244,6 +244,12 @@ def test_attention(driver, tmp_path, dim, page, heads, group, lengths, counts, d
     attend(driver, tmp_path, dim, page, heads, group, lengths, counts, dtype)
 
 
+def test_attention_of_more_rows_than_a_wave_has_lanes(driver, tmp_path):
+    lengths = [0] * 70
+    lengths[3], lengths[64], lengths[69] = 40, 300, 5
+    attend(driver, tmp_path, 64, 32, 1, 1, lengths, [0, 0, 0, 1] + [0] * 60 + [20, 0, 0, 0, 0, 2], 1, per_row=10)
+
+
 def test_attention_without_causality(driver, tmp_path):
     attend(driver, tmp_path, 64, 32, 1, 2, [45, 130], [20, 3], 0, causal=0)
 
