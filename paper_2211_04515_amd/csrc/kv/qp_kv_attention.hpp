@@ -45,18 +45,18 @@ constexpr uint32_t kAtStep = 32;                 // tokens of a wave's step
 constexpr uint32_t kAtTile = kAtStep * kAtWaves; // tokens that work is counted in
 constexpr uint32_t kAtUnit = 16;                 // columns that partial results are counted in
 template <bool MANY> constexpr uint32_t kAtCols = MANY ? 128u : kAtUnit;     // columns of an item
-// pieces that a call is cut into, and tiles that one has at least (joining costs a kernel and a pass over the pieces, more than
-// it takes to go through these)
+// Blocks that run at the same time: a call is cut into no more pieces than that, if it can be.
 #ifndef QP_KV_FEW
-#define QP_KV_FEW 512
+#define QP_KV_FEW 768
 #endif
 #ifndef QP_KV_MANY
-#define QP_KV_MANY 320
+#define QP_KV_MANY 512
 #endif
+template <bool MANY> constexpr uint32_t kAtSlots = MANY ? QP_KV_MANY : QP_KV_FEW;     // at most: three, two blocks a CU
+// Tiles that a piece has at least: joining costs a kernel and a pass over the pieces, more than it takes to go through these.
 #ifndef QP_KV_LEAST
 #define QP_KV_LEAST 4
 #endif
-template <bool MANY> constexpr uint32_t kAtTarget = MANY ? QP_KV_MANY : QP_KV_FEW;
 constexpr uint32_t kAtLeast = QP_KV_LEAST;
 constexpr float kAtHeadroom = 8.0f;              // log2 that a score may lie above its column's m
 
@@ -72,6 +72,7 @@ struct AtWork {
     float *nums;
     uint32_t most_cols, most_units;
     uint32_t wide;                               // rows are cut into 128 columns first
+    uint32_t slots;                              // blocks that run at the same time
 };
 constexpr size_t kAtHeader = 256;
 // Columns that a wave of `few` shall not take one by one: see above.
@@ -82,17 +83,17 @@ template <bool MANY> uint64_t at_items(const KvLayer &c, uint32_t group)     // 
     if (!MANY && at_wide(group, c.rows, c.tokens)) return c.kv_heads * rows;
     return c.kv_heads * ((uint64_t)c.tokens * group / kAtCols<MANY> + rows);
 }
-// An item of n tiles is cut up if n exceeds a piece's share, and then into less than n / share + 1 <= 2 n / share pieces: twice
-// the target at most for all of them, in target items at most.
+// The items that are cut up have 2 kAtSlots pieces together at most, see at_share, so there are kAtSlots of them at most.
 template <bool MANY> AtWork at_work(char *ws, const KvLayer &c, uint32_t dim, uint32_t group, size_t &bytes)
 {
     const uint64_t tiles = (((uint64_t)c.pages_per_row << c.page_shift) + kAtTile - 1u) / kAtTile, items = at_items<MANY>(c, group);
-    const uint64_t columns = (uint64_t)c.tokens * c.kv_heads * group, target = kAtTarget<MANY>;
-    uint64_t pieces = tiles <= kAtLeast ? 0u : 2u * target, cols = tiles <= kAtLeast ? 0u : target * kAtCols<MANY>;
-    if (items < 2u * target && items * tiles < pieces) pieces = items * tiles;
+    const uint64_t columns = (uint64_t)c.tokens * c.kv_heads * group, slots = kAtSlots<MANY>;
+    uint64_t pieces = tiles <= kAtLeast ? 0u : 2u * slots, cols = tiles <= kAtLeast ? 0u : slots * kAtCols<MANY>;
+    if (items < 2u * slots && items * tiles < pieces) pieces = items * tiles;
     if (columns < cols) cols = columns;
     AtWork w{};
     w.wide = at_wide(group, c.rows, c.tokens) ? 1u : 0u;
+    w.slots = kAtSlots<MANY>;
     w.most_units = (uint32_t)(pieces * (kAtCols<MANY> / kAtUnit));
     w.most_cols = (uint32_t)cols;
     const size_t sums = kAtHeader + (size_t)cols * sizeof(u32x4), nums = sums + (size_t)w.most_units * kAtUnit * sizeof(float2);
@@ -207,19 +208,30 @@ template <bool MANY> struct AtParts {
         return f;
     }
 };
-template <bool MANY> __device__ __forceinline__ uint32_t at_share(const KvLayer &c, uint64_t cost)
+// Tiles that a piece should have.  The pieces of a call are to run in one round, so there should be `slots` of them but no more (a piece
+// too many makes a second round: attend_batch 33.6 us with 768 pieces, 39.8 with 800), in two rounds where the items alone are more;
+// with yet more items only what is longer than a slot's share is cut.  `count(per)`: the pieces that come of a share.
+// Either count(per) <= 2 slots, or per > 2 cost / slots (the steps below more than double per, and from then on an item of n tiles
+// in more than one piece has less than 2 n / per): 2 slots pieces at most come of items that are cut.
+template <typename Count> __device__ __forceinline__ uint32_t at_share(uint64_t cost, uint64_t items, uint32_t slots, const Count &count)
 {
-    return (uint32_t)min(max((cost * c.kv_heads + kAtTarget<MANY> - 1u) / kAtTarget<MANY>, (uint64_t)kAtLeast), (uint64_t)0x7fffffffu);
+    const uint64_t goal = items <= slots ? slots : items <= 2u * slots ? 2u * slots : slots;
+    uint32_t per = (uint32_t)min(max((cost + goal - 1u) / goal, (uint64_t)kAtLeast), (uint64_t)0x3fffffffu);
+    if (items <= 2u * slots)
+        for (int i = 0; i < 20 && count(per) > goal; ++i) per += max(1u, per / 16u);
+    return per;
 }
 
 // False: the call has fewer pieces than blocks.
 template <bool MANY> __device__ __forceinline__ bool at_find(const KvLayer &c, const KvAttn &a, const AtWork &w, uint32_t block, AtPiece &mine)
 {
     const uint32_t tid = threadIdx.x, lane = tid % kWave;
-    const AtRow none{KvRow{0, 0, 0}, 0u, 0u, 0u, 1u};
+    AtRow none{};
+    none.tiles = 1u;
     if (c.rows <= (uint32_t)kWave) {             // every wave for itself, a row a lane: nothing to wait for but the lengths
         const AtRow o = lane < c.rows ? at_row<MANY>(c, a, w.wide, lane) : none;
-        const uint32_t per = at_share<MANY>(c, at_wave_sum((uint64_t)o.tiles * o.items));
+        const uint64_t cost = at_wave_sum((uint64_t)o.tiles * o.items) * c.kv_heads, items = (uint64_t)wave_sum_u32(o.items) * c.kv_heads;
+        const uint32_t per = at_share(cost, items, w.slots, [&](uint32_t p) { return (uint64_t)wave_sum_u32(o.items * ((o.tiles + p - 1u) / p)) * c.kv_heads; });
         const AtParts<MANY> parts(c, o, per);
         uint32_t e[3] = {parts.blocks, parts.units, parts.cols};
 #pragma unroll
@@ -259,7 +271,8 @@ template <bool MANY> __device__ __forceinline__ bool at_find(const KvLayer &c, c
     if (lane == 0u) work[tid / kWave] = cost;
     if (tid == 0u) have = split = 0u;
     __syncthreads();
-    const uint32_t per = at_share<MANY>(c, work[0] + work[1] + work[2] + work[3]);
+    // (many rows: their mean piece is taken for what is lost at their ends)
+    const uint32_t per = at_share((work[0] + work[1] + work[2] + work[3]) * c.kv_heads * 5u / 4u, 4u * (uint64_t)w.slots, w.slots, [](uint32_t) { return 0ull; });
     uint32_t before[3] = {0u, 0u, 0u};                   // blocks, units, columns of the rows so far
     for (uint32_t r0 = 0; r0 < c.rows; r0 += kAtThreads) {
         const uint32_t r = r0 + tid;
@@ -991,7 +1004,7 @@ __device__ __forceinline__ float at_wave_sum(float v)
 template <int D, int DT> __global__ __launch_bounds__(kAtThreads) void k_kv_join(KvView out, uint32_t q_heads, AtWork few, AtWork many)
 {
     constexpr int PER = (D + kWave - 1) / kWave;
-    constexpr uint32_t kMost = 2u * (kAtTarget<false> > kAtTarget<true> ? kAtTarget<false> : kAtTarget<true>);
+    constexpr uint32_t kMost = 2u * (kAtSlots<false> > kAtSlots<true> ? kAtSlots<false> : kAtSlots<true>);
     __shared__ float weight[kMost];
     __shared__ float part[kAtWaves][D], top_of[kAtWaves], sum_of[kAtWaves];
     const uint32_t tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
@@ -1081,15 +1094,19 @@ static hipError_t at_launch(const KvLayer &c, const KvView &q, const KvView &out
     const bool wide = at_wide(a.group, c.rows, c.tokens);
     size_t few_bytes, bytes;
     (void)at_bytes(c, D, a.group, few_bytes);
-    const AtWork few = at_work<false>(ws, c, D, a.group, bytes);
-    const AtWork many = wide ? at_work<true>(ws + few_bytes, c, D, a.group, bytes) : AtWork{};
-    // the target's pieces, and one more for each item at most
+    AtWork few = at_work<false>(ws, c, D, a.group, bytes);
+    AtWork many = wide ? at_work<true>(ws + few_bytes, c, D, a.group, bytes) : AtWork{};
+    if (D == 256 || (D == 128 && DT == QP_F32)) {      // their registers leave room for a block less a CU
+        few.slots = kAtSlots<false> * 2u / 3u;
+        many.slots = kAtSlots<true> / 2u;
+    }
+    // (pieces: see at_share; an item that is not cut up is one)
     hipError_t e;
     if (wide) {
-        hipLaunchKernelGGL((k_kv_attention_many<D, DT>), dim3((unsigned)(kAtTarget<true> + at_items<true>(c, a.group))), dim3(kAtThreads), 0, s, c, q, out, a, many);
+        hipLaunchKernelGGL((k_kv_attention_many<D, DT>), dim3((unsigned)(2u * kAtSlots<true> + at_items<true>(c, a.group))), dim3(kAtThreads), 0, s, c, q, out, a, many);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((k_kv_attention_few<D, DT>), dim3((unsigned)(kAtTarget<false> + at_items<false>(c, a.group))), dim3(kAtThreads), 0, s, c, q, out, a, few);
+    hipLaunchKernelGGL((k_kv_attention_few<D, DT>), dim3((unsigned)(2u * kAtSlots<false> + at_items<false>(c, a.group))), dim3(kAtThreads), 0, s, c, q, out, a, few);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const uint32_t cols = few.most_cols + many.most_cols;
     if (cols == 0u) return hipSuccess;        // no row is longer than a piece
