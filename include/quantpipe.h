@@ -451,8 +451,8 @@ size_t qp_kv_page_bytes(const qp_kv_cache_t *cache);
 /* ---- pages: handing out, sharing, freeing, moving together -----------------------------
  * The pool record is int32 words in device memory: QP_KV_POOL_HEADER of header, then refs[n_pages], how many rows hold each page
  * (0 = free), then room that the calls work in.  Header word 0: pages that the last qp_kv_reserve was short of (0: it was done);
- * word 1: rows of the last qp_kv_reserve that would have outgrown pages_per_row; word 2: rows that the last qp_kv_fork
- * refused; word 3: pages in use after the last qp_kv_compact.  qp_kv_pool_init makes every page free (do it once; it also clears
+ * word 1: rows of the last qp_kv_reserve that would have outgrown pages_per_row; word 2: rows that qp_kv_fork has refused so
+ * far (it only adds; the caller may clear it); word 3: pages in use after the last qp_kv_compact.  qp_kv_pool_init makes every page free (do it once; it also clears
  * the room that the calls need cleared between them, and they leave it so).  A row holds a page for each page_tokens
  * tokens begun: a length of 0 is a row that holds none. */
 size_t qp_kv_pool_bytes(uint32_t n_pages);                     /* 4 * (16 + 6 n_pages); 0 if n_pages is refused */
@@ -466,7 +466,7 @@ qp_status qp_kv_reserve(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, co
                         size_t pool_bytes, void *stream);
 /* parent_dev[r] >= 0: row r, which must be empty, becomes a copy of row parent_dev[r] that shares its pages (nothing is copied
  * until one of them grows).  A row that is not empty, is its own parent, or names a parent that is out of range or is itself forked
- * in this call is left as it is and counted in header word 2. */
+ * in this call is left as it is and added to header word 2. */
 qp_status qp_kv_fork(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, const int32_t *parent_dev, void *pool_dev,
                      size_t pool_bytes, void *stream);
 /* keep_dev[r] >= 0: row r keeps its first keep_dev[r] tokens (0: none, the row is freed; drafted tokens that were rejected go the same

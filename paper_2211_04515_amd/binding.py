@@ -503,7 +503,7 @@ def qp_kv_reserve(cache, rows, pool, want, stream=None) -> None:
 
 
 def qp_kv_fork(cache, rows, pool, parent, stream=None) -> None:
-    """Row r becomes a copy of row parent[r] (negative: left alone) that shares its pages; word 2 of `pool` counts refused rows."""
+    """Row r becomes a copy of row parent[r] (negative: left alone) that shares its pages; word 2 of `pool` counts the rows refused so far."""
     _books("qp_kv_fork", cache, rows, pool, parent, stream)
 
 

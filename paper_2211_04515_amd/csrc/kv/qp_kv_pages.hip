@@ -27,25 +27,27 @@ __device__ __forceinline__ int64_t kv_length(const qp_kv_rows_t &rows, uint32_t 
 }
 
 // Inclusive prefix sum over the block's 1024 lanes; total: of all of them.  `part` holds one sum a wave.
-__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *part, uint32_t &total)
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x)
 {
-    const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    uint32_t x = v;
+    const uint32_t lane = threadIdx.x % kWave;
 #pragma unroll
     for (uint32_t d = 1; d < (uint32_t)kWave; d *= 2u) {
         const uint32_t o = __shfl_up(x, d, kWave);
         if (lane >= d) x += o;
     }
+    return x;
+}
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *part, uint32_t &total)
+{
+    const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const uint32_t x = wave_scan(v);
     __syncthreads();                          // (the sums of an earlier scan have been read)
     if (lane == kWave - 1u) part[wave] = x;
     __syncthreads();
-    uint32_t before = 0;
-    total = 0;
-    for (uint32_t w = 0; w < (uint32_t)(kKvPlan / kWave); ++w) {
-        before += w < wave ? part[w] : 0u;
-        total += part[w];
-    }
-    return x + before;
+    const uint32_t sums = wave_scan(lane < (uint32_t)(kKvPlan / kWave) ? part[lane] : 0u);     // (every wave adds the 16 up for itself)
+    total = (uint32_t)__builtin_amdgcn_readlane((int)sums, kKvPlan / kWave - 1);
+    const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)sums, (int)(wave ? wave - 1u : 0u));
+    return x + (wave ? before : 0u);
 }
 
 __global__ __launch_bounds__(256) void k_kv_pool_init(int32_t *pool, uint32_t words)
@@ -54,9 +56,11 @@ __global__ __launch_bounds__(256) void k_kv_pool_init(int32_t *pool, uint32_t wo
 }
 
 // ---- pages that move: pairs {from, to}, in every layer ---------------------------------------------------------------------
-__global__ __launch_bounds__(kKvCopyThreads) void k_kv_move(KvPages c, const int32_t *__restrict__ header, const int32_t *__restrict__ pairs)
+// (`went`: what a compaction has noted at the pages that move, cleared here for the next call; zero already after a reservation.)
+__global__ __launch_bounds__(kKvCopyThreads) void k_kv_move(KvPages c, const int32_t *__restrict__ header, const int32_t *__restrict__ pairs, int32_t *went)
 {
     const uint32_t count = (uint32_t)header[kKvMoves];
+    for (uint32_t i = blockIdx.x * kKvCopyThreads + threadIdx.x; i < count; i += gridDim.x * kKvCopyThreads) went[pairs[2u * i]] = 0;
     const uint32_t tiles = (uint32_t)((c.page_bytes + kKvCopyTile - 1u) / kKvCopyTile);      // of a page
     const uint64_t work = (uint64_t)count * c.layers * tiles;
     for (uint64_t i = blockIdx.x; i < work; i += gridDim.x) {
@@ -81,54 +85,70 @@ __global__ __launch_bounds__(kKvCopyThreads) void k_kv_move(KvPages c, const int
 }
 
 // ---- reserve -----------------------------------------------------------------------------------------------------------
-// What a row asks for: `fresh` pages for the slots from `slot` on, the first of them in the place of a shared page if `copy`.
+// A row of the call: its length, what it wants, and the page that it writes next if others hold that too (else -1).
+struct KvWish {
+    int64_t length;
+    int32_t want, shared;
+};
+__device__ __forceinline__ KvWish kv_wish(const qp_kv_rows_t &rows, const KvPages &c, const KvPool &p, const int32_t *want, uint32_t r)
+{
+    KvWish o{kv_length(rows, r, c.page_shift), want[r], -1};
+    if (o.want <= 0 || (o.length & ((1 << c.page_shift) - 1)) == 0) return o;
+    const int32_t page = rows.table_dev[(uint64_t)r * rows.pages_per_row + (uint64_t)(o.length >> c.page_shift)];
+    if ((uint32_t)page < c.n_pages && p.refs[page] > 1) o.shared = page;
+    return o;
+}
+// What it asks for: `fresh` pages for the slots from `slot` on, the first of them in the place of the shared page if `copy`.
 struct KvAsk {
     uint32_t slot, fresh;
-    int32_t shared;          // the page that is written next, if others hold it too; else -1
     bool copy;
 };
-__device__ __forceinline__ int32_t kv_next_page(const qp_kv_rows_t &rows, const KvPages &c, const KvPool &p, uint32_t r, int64_t len, int32_t want)
-{
-    if (want <= 0 || (len & ((1 << c.page_shift) - 1)) == 0) return -1;
-    const int32_t page = rows.table_dev[(uint64_t)r * rows.pages_per_row + (uint64_t)(len >> c.page_shift)];
-    return (uint32_t)page < c.n_pages && p.refs[page] > 1 ? page : -1;
-}
-__device__ __forceinline__ KvAsk kv_ask(const qp_kv_rows_t &rows, const KvPages &c, const KvPool &p, uint32_t r, int64_t len, int32_t want)
+__device__ __forceinline__ KvAsk kv_ask(const KvPages &c, const KvPool &p, uint32_t r, const KvWish &w)
 {
     KvAsk a;
-    a.slot = (uint32_t)(len >> c.page_shift);
-    a.shared = kv_next_page(rows, c, p, r, len, want);
-    // if every holder of the page asks, the last row among them keeps it: what serving them in turn comes to
+    // If every holder of the page asks, the last row among them keeps it: what serving them in turn comes to.
     // (count and last are this kernel's atomics: read where those are, not through a cache line fetched before them)
-    a.copy = a.shared >= 0 && !(ld_dev(reinterpret_cast<uint32_t *>(p.count + a.shared)) == (uint32_t)p.refs[a.shared] &&
-                                ld_dev(reinterpret_cast<uint32_t *>(p.last + a.shared)) == r + 1u);
-    a.fresh = want > 0 ? kv_pages_of(len + want, c.page_shift) - kv_pages_of(len, c.page_shift) + (a.copy ? 1u : 0u) : 0u;
-    if (!a.copy) a.slot = kv_pages_of(len, c.page_shift);
+    a.copy = w.shared >= 0 && !(ld_dev(reinterpret_cast<uint32_t *>(p.count + w.shared)) == (uint32_t)p.refs[w.shared] &&
+                                ld_dev(reinterpret_cast<uint32_t *>(p.last + w.shared)) == r + 1u);
+    a.fresh = w.want > 0 ? kv_pages_of(w.length + w.want, c.page_shift) - kv_pages_of(w.length, c.page_shift) + (a.copy ? 1u : 0u) : 0u;
+    a.slot = a.copy ? (uint32_t)(w.length >> c.page_shift) : kv_pages_of(w.length, c.page_shift);
     return a;
 }
 
+// Latency is all that it costs: a lane keeps its first row's wish and ask in registers (most calls have no more rows than lanes), so
+// that what it reads is read once: 15.5 -> RESERVE_US us for 40 rows.
 __global__ __launch_bounds__(kKvPlan) void k_kv_reserve(KvPages c, qp_kv_rows_t rows, const int32_t *__restrict__ want, void *pool)
 {
     __shared__ uint32_t part[kKvPlan / kWave];
     __shared__ uint32_t ask_fresh[kKvPlan], ask_slot[kKvPlan], ask_base[kKvPlan];
     const uint32_t tid = threadIdx.x;
     const KvPool p = kv_pool(pool, c.n_pages);
+    const KvWish nothing{0, 0, -1};
+    const KvWish first = tid < rows.rows ? kv_wish(rows, c, p, want, tid) : nothing;
+    const auto wish = [&](uint32_t r) { return r == tid ? first : kv_wish(rows, c, p, want, r); };
+    // the free pages among the first, on their way while the rows are looked at
+    uint32_t bits0 = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < (uint32_t)kKvScan; ++i) bits0 |= (tid * kKvScan + i < c.n_pages && p.refs[tid * kKvScan + i] == 0 ? 1u : 0u) << i;
     // how many of a shared page's holders write into it next, and the last of them
     for (uint32_t r = tid; r < rows.rows; r += kKvPlan) {
-        const int32_t page = kv_next_page(rows, c, p, r, kv_length(rows, r, c.page_shift), want[r]);
+        const int32_t page = wish(r).shared;
         if (page >= 0) {
             atomicAdd(reinterpret_cast<uint32_t *>(p.count + page), 1u);
             atomicMax(reinterpret_cast<uint32_t *>(p.last + page), r + 1u);
         }
     }
     __syncthreads();
+    const KvAsk none{0u, 0u, false};
+    const KvAsk first_ask = tid < rows.rows ? kv_ask(c, p, tid, first) : none;
+    const auto ask = [&](uint32_t r) { return r == tid ? first_ask : kv_ask(c, p, r, wish(r)); };
+    const int64_t cap = (int64_t)rows.pages_per_row << c.page_shift;
     uint64_t need = 0;
     uint32_t over = 0;
     for (uint32_t r = tid; r < rows.rows; r += kKvPlan) {
-        const int64_t len = kv_length(rows, r, c.page_shift);
-        const int32_t w = want[r];
-        if (w > 0 && len + w > ((int64_t)rows.pages_per_row << c.page_shift)) ++over;
-        else need += kv_ask(rows, c, p, r, len, w).fresh;
+        const KvWish w = wish(r);
+        if (w.want > 0 && w.length + w.want > cap) ++over;
+        else need += ask(r).fresh;
     }
     uint32_t rows_over = 0, low = 0, high = 0;
     block_scan(over, part, rows_over);
@@ -139,13 +159,13 @@ __global__ __launch_bounds__(kKvPlan) void k_kv_reserve(KvPages c, qp_kv_rows_t 
     uint32_t found = 0;
     for (uint32_t p0 = 0; p0 < c.n_pages && found < total && rows_over == 0u; p0 += kKvPlan * kKvScan) {
         const uint32_t at = p0 + tid * kKvScan;
-        uint32_t mine = 0, bits = 0;
+        uint32_t bits = bits0;
+        if (p0 != 0u) {
+            bits = 0;
 #pragma unroll
-        for (uint32_t i = 0; i < (uint32_t)kKvScan; ++i) {
-            const bool free = at + i < c.n_pages && p.refs[at + i] == 0;
-            bits |= (free ? 1u : 0u) << i;
-            mine += free ? 1u : 0u;
+            for (uint32_t i = 0; i < (uint32_t)kKvScan; ++i) bits |= (at + i < c.n_pages && p.refs[at + i] == 0 ? 1u : 0u) << i;
         }
+        const uint32_t mine = (uint32_t)__popcll(bits);
         uint32_t sum = 0;
         uint32_t place = found + block_scan(mine, part, sum) - mine;
         for (uint32_t i = 0; i < (uint32_t)kKvScan; ++i)
@@ -161,9 +181,8 @@ __global__ __launch_bounds__(kKvPlan) void k_kv_reserve(KvPages c, qp_kv_rows_t 
     for (uint32_t r0 = 0; r0 < rows.rows && done; r0 += kKvPlan) {
         const uint32_t r = r0 + tid;
         const bool is = r < rows.rows;
-        const int64_t len = is ? kv_length(rows, r, c.page_shift) : 0;
-        const int32_t w = is ? want[r] : 0;
-        const KvAsk a = is ? kv_ask(rows, c, p, r, len, w) : KvAsk{0u, 0u, -1, false};
+        const KvWish w = is ? wish(r) : nothing;
+        const KvAsk a = is ? ask(r) : none;
         uint32_t sum = 0, copies = 0;
         const uint32_t mine = base + block_scan(a.fresh, part, sum) - a.fresh;
         const uint32_t move = moves + block_scan(a.copy ? 1u : 0u, part, copies) - (a.copy ? 1u : 0u);
@@ -171,16 +190,14 @@ __global__ __launch_bounds__(kKvPlan) void k_kv_reserve(KvPages c, qp_kv_rows_t 
         ask_slot[tid] = a.slot;
         ask_base[tid] = mine;
         if (a.copy) {
-            p.pairs[2u * move] = a.shared;
+            p.pairs[2u * move] = w.shared;
             p.pairs[2u * move + 1u] = p.list[mine];
         }
         __syncthreads();                      // every row of these has looked at the counts and the table
-        if (is && w > 0) rows.lengths_dev[r] = (int32_t)(len + w);
-        for (uint32_t k = tid / kWave; k < (uint32_t)kKvPlan; k += kKvPlan / kWave)   // a wave a row: its pages
-            for (uint32_t i = tid % kWave; i < ask_fresh[k]; i += kWave) {
-                const int32_t page = p.list[ask_base[k] + i];
-                rows.table_dev[(uint64_t)(r0 + k) * rows.pages_per_row + ask_slot[k] + i] = page;
-            }
+        if (is && w.want > 0) rows.lengths_dev[r] = (int32_t)(w.length + w.want);
+        for (uint32_t k = tid / kWave; k < min((uint32_t)kKvPlan, rows.rows - r0); k += kKvPlan / kWave)   // a wave a row: its pages
+            for (uint32_t i = tid % kWave; i < ask_fresh[k]; i += kWave)
+                rows.table_dev[(uint64_t)(r0 + k) * rows.pages_per_row + ask_slot[k] + i] = p.list[ask_base[k] + i];
         base += sum;
         moves += copies;
         __syncthreads();
@@ -191,7 +208,8 @@ __global__ __launch_bounds__(kKvPlan) void k_kv_reserve(KvPages c, qp_kv_rows_t 
         for (uint32_t i = tid; i < moves; i += kKvPlan) atomicAdd(reinterpret_cast<uint32_t *>(p.refs + p.pairs[2u * i]), 0xffffffffu);
     }
     for (uint32_t i = tid; i < moves; i += kKvPlan) p.count[p.pairs[2u * i]] = p.last[p.pairs[2u * i]] = 0;
-    for (uint32_t r = tid; r < rows.rows; r += kKvPlan) {   // (a counted page that was not copied is still its rows' next one)
+    if (tid < rows.rows && first.shared >= 0) p.count[first.shared] = p.last[first.shared] = 0;
+    for (uint32_t r = tid + kKvPlan; r < rows.rows; r += kKvPlan) {   // (a counted page that was not copied is still its row's next one)
         const int64_t len = kv_length(rows, r, c.page_shift) - (done && want[r] > 0 ? want[r] : 0);
         if (want[r] <= 0 || (len & ((1 << c.page_shift) - 1)) == 0) continue;
         const int32_t page = rows.table_dev[(uint64_t)r * rows.pages_per_row + (uint64_t)(len >> c.page_shift)];
@@ -227,7 +245,6 @@ __global__ __launch_bounds__(256) void k_kv_fork(KvPages c, qp_kv_rows_t rows, c
     }
     if (threadIdx.x == 0u) rows.lengths_dev[r] = (int32_t)len;
 }
-__global__ void k_kv_fork_begin(void *pool) { static_cast<int32_t *>(pool)[kKvRefused] = 0; }
 
 __global__ __launch_bounds__(256) void k_kv_free(KvPages c, qp_kv_rows_t rows, const int32_t *__restrict__ keep, void *pool)
 {
@@ -307,13 +324,6 @@ __global__ __launch_bounds__(256) void k_kv_renumber(KvPages c, qp_kv_rows_t row
         if ((uint32_t)*entry < c.n_pages && p.count[*entry] > 0) *entry = p.count[*entry] - 1;
     }
 }
-__global__ __launch_bounds__(256) void k_kv_compact_end(KvPages c, void *pool)
-{
-    const KvPool p = kv_pool(pool, c.n_pages);
-    const uint32_t moves = (uint32_t)p.header[kKvMoves];
-    for (uint32_t i = blockIdx.x * 256u + threadIdx.x; i < moves; i += gridDim.x * 256u) p.count[p.pairs[2u * i]] = 0;
-}
-
 static dim3 blocks_for(uint64_t items, uint32_t per, uint32_t most)
 {
     const uint64_t b = (items + per - 1u) / per;
@@ -337,15 +347,12 @@ hipError_t launch_kv_reserve(const KvPages &c, const qp_kv_rows_t &rows, const i
     hipLaunchKernelGGL(k_kv_reserve, dim3(1), dim3(kKvPlan), 0, s, c, rows, want, pool);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_kv_move, move_blocks(c, rows.rows), dim3(kKvCopyThreads), 0, s, c, p.header, p.pairs);
+    hipLaunchKernelGGL(k_kv_move, move_blocks(c, rows.rows), dim3(kKvCopyThreads), 0, s, c, p.header, p.pairs, p.count);
     return hipGetLastError();
 }
 
 hipError_t launch_kv_fork(const KvPages &c, const qp_kv_rows_t &rows, const int32_t *parent, void *pool, hipStream_t s)
 {
-    hipLaunchKernelGGL(k_kv_fork_begin, dim3(1), dim3(1), 0, s, pool);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k_kv_fork, dim3(rows.rows), dim3(256), 0, s, c, rows, parent, pool);
     return hipGetLastError();
 }
@@ -362,11 +369,9 @@ hipError_t launch_kv_compact(const KvPages &c, const qp_kv_rows_t &rows, void *p
     hipLaunchKernelGGL(k_kv_compact, dim3(1), dim3(kKvPlan), 0, s, c, pool);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_kv_move, move_blocks(c, c.n_pages), dim3(kKvCopyThreads), 0, s, c, p.header, p.pairs);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL(k_kv_renumber, dim3(rows.rows), dim3(256), 0, s, c, rows, pool);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(k_kv_compact_end, blocks_for(c.n_pages, 256u, 256u), dim3(256), 0, s, c, pool);
+    hipLaunchKernelGGL(k_kv_move, move_blocks(c, c.n_pages), dim3(kKvCopyThreads), 0, s, c, p.header, p.pairs, p.count);
     return hipGetLastError();
 }
 

@@ -82,35 +82,54 @@ template <int DT> __device__ __forceinline__ void kv_store8(unsigned char *p, ui
 
 // The tokens of a call that one step of a wave takes: token t of the call is the first of them.
 struct KvOctet {
-    int32_t row, slot;       // slot: of the first token's page
+    uint32_t slot;           // of the first token's page
     uint32_t tg;             // the page's group of eight
     uint32_t j0, count;      // tokens j0 .. j0 + count - 1 of the group
     int32_t next;            // the call's token behind them
+    bool starts;             // the first of the call's tokens in that group
 };
-
-// From token t on: the tokens of t's row that share its group.  `first` says which position each row's first token has; false: token
-// t is not stored anywhere.
-template <typename First>
-__device__ __forceinline__ bool kv_octet(const KvLayer &c, int32_t t, const First &first, KvOctet &o, int32_t &begin, int32_t &at_begin)
-{
-    o.next = t + 1;
-    const int32_t found = kv_find_row(c, t);
-    const int32_t r = __builtin_amdgcn_readfirstlane(found);
-    if (r < 0) return false;
-    const KvRow row = kv_row(c, (uint32_t)r);
-    if (t < row.begin || t >= row.begin + row.count) return false;   // token_begin does not ascend
-    const int64_t pos = (int64_t)first((uint32_t)r, row) + (t - row.begin);
-    begin = row.begin;
-    at_begin = first((uint32_t)r, row);
-    if (pos < 0 || pos >= (int64_t)(c.pages_per_row << c.page_shift)) return false;
-    o.row = r;
-    o.j0 = (uint32_t)pos & 7u;
-    o.count = min(8u - o.j0, (uint32_t)(row.begin + row.count - t));
-    o.next = t + (int32_t)o.count;
-    o.slot = (int32_t)((uint32_t)pos >> c.page_shift);
-    o.tg = ((uint32_t)pos & ((1u << c.page_shift) - 1u)) >> 3;
-    return true;
-}
+// A walk over the call's tokens [t, end): the row that the last one was in is kept, and so is the page.
+struct KvWalk {
+    KvRow row;
+    int32_t r, at;           // the row, or -1; the position of its first token
+    uint32_t slot;
+    int32_t page;
+    __device__ __forceinline__ KvWalk() : row{0, 0, 0}, r(-1), at(0), slot(0xffffffffu), page(-1) {}
+    // From token t on: the tokens of t's row that share its group.  `first(r, row)`: the position of a row's first token.  False: token t has
+    // no place (r < 0: it is no row's).
+    template <typename First> __device__ __forceinline__ bool octet(const KvLayer &c, int32_t t, const First &first, KvOctet &o)
+    {
+        o.next = t + 1;
+        if (r < 0 || t < row.begin || t >= row.begin + row.count) {
+            r = __builtin_amdgcn_readfirstlane(kv_find_row(c, t));
+            slot = 0xffffffffu;
+            if (r < 0) return false;
+            row = kv_row(c, (uint32_t)r);
+            at = first((uint32_t)r, row);
+            if (t < row.begin || t >= row.begin + row.count) {       // token_begin does not ascend
+                r = -1;
+                return false;
+            }
+        }
+        const int64_t pos = (int64_t)at + (t - row.begin);
+        if (pos < 0 || pos >= (int64_t)(c.pages_per_row << c.page_shift)) return false;
+        o.j0 = (uint32_t)pos & 7u;
+        o.count = min(8u - o.j0, (uint32_t)(row.begin + row.count - t));
+        o.next = t + (int32_t)o.count;
+        o.slot = (uint32_t)pos >> c.page_shift;
+        o.tg = ((uint32_t)pos & ((1u << c.page_shift) - 1u)) >> 3;
+        o.starts = o.j0 == 0u || t == row.begin;         // (a token ahead of the row's start has no place, and the next one is the group's first)
+        return true;
+    }
+    __device__ __forceinline__ int32_t page_of(const KvLayer &c, const KvOctet &o)
+    {
+        if (o.slot != slot) {
+            slot = o.slot;
+            page = kv_page(c, (uint32_t)r, slot);
+        }
+        return page;
+    }
+};
 
 // ---- quantize ----------------------------------------------------------------------------------------------------------
 struct KvGrid {
@@ -167,15 +186,14 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvLayer c, KvView k, K
     if (t0 >= c.tokens) return;
     const int32_t end = (int32_t)min(t0 + span, (uint64_t)c.tokens);
     const auto first = [](uint32_t, const KvRow &row) { return row.length - row.count; };
+    KvWalk walk;
     for (int32_t t = (int32_t)t0; t < end;) {
         KvOctet o;
-        int32_t begin, at_begin;
-        const bool good = kv_octet(c, t, first, o, begin, at_begin);
+        const bool good = walk.octet(c, t, first, o);
         const int32_t here = t;
         t = o.next;
-        // an octet is taken where it begins: at a group's first token, or at the row's first that has a place
-        if (!good || (o.j0 != 0u && here != begin + max(0, -at_begin))) continue;
-        const int32_t page = kv_page(c, (uint32_t)o.row, (uint32_t)o.slot);
+        if (!good || !o.starts) continue;        // an octet is taken where it begins
+        const int32_t page = walk.page_of(c, o);
         if (page < 0) continue;
         unsigned char *slab = kv_slab(c, page, head);
         const uint32_t pt = 1u << c.page_shift;
@@ -229,27 +247,27 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_read(KvLayer c, const int32_t
     if (t0 >= c.tokens) return;
     const int32_t end = (int32_t)min(t0 + span, (uint64_t)c.tokens);
     const auto first = [firsts](uint32_t r, const KvRow &) { return firsts ? firsts[r] : 0; };
+    KvWalk walk;
     for (int32_t t = (int32_t)t0; t < end;) {
         KvOctet o;
-        int32_t begin = -1, at_begin = 0;
-        const bool good = kv_octet(c, t, first, o, begin, at_begin);
+        const bool good = walk.octet(c, t, first, o);
         const int32_t here = t;
         t = o.next;
         if (!good) {
-            if (begin < 0) continue;         // the token is no row's
+            if (walk.r < 0) continue;        // the token is no row's
             o.j0 = 0u;                       // a place outside the table: this token alone, zeros
             o.count = 1u;
-        } else if (o.j0 != 0u && here != begin + max(0, -at_begin)) {
+        } else if (!o.starts) {
             continue;
         }
-        const int32_t page = good ? kv_page(c, (uint32_t)o.row, (uint32_t)o.slot) : -1;
+        const int32_t page = good ? walk.page_of(c, o) : -1;
         const bool mine = j >= o.j0 && j < o.j0 + o.count;
         const uint64_t tok = mine ? (uint64_t)here + (j - o.j0) : (uint64_t)here;
         unsigned char *kp = k.data + tok * k.token_stride + head * k.head_stride;
         unsigned char *vp = v.data + tok * v.token_stride + head * v.head_stride;
         const float zero[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        const int64_t pos = (int64_t)at_begin + ((int64_t)here - begin) + ((int64_t)j - o.j0);
-        const bool there = page >= 0 && mine && pos < (int64_t)kv_row(c, (uint32_t)o.row).length;
+        const int64_t pos = (int64_t)walk.at + ((int64_t)here - walk.row.begin) + ((int64_t)j - o.j0);
+        const bool there = page >= 0 && mine && pos < (int64_t)walk.row.length;
         if (page < 0) {
 #pragma unroll
             for (int u = 0; u < UNITS; ++u)
@@ -290,9 +308,17 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_read(KvLayer c, const int32_t
     }
 }
 
-// A wave looks through eight tokens where rows bring eight or more on average, else through one: with single tokens every
-// octet is a token of its own, and eight of them one after the other would take eight times the latency.
-static uint32_t kv_span(const KvLayer &c) { return c.tokens >= 8u * (uint64_t)c.rows ? 8u : 1u; }
+// A wave looks through one token where rows bring fewer than eight on average: with single tokens every octet is a token of its own, and
+// eight of them one after the other would take eight times the latency.  Else through eight, an octet's worth, as long as that fills the
+// chip, and through 32 where that still does: the row is found once for four octets.
+#ifndef QP_KV_SPAN_FILL
+#define QP_KV_SPAN_FILL (256u * 32u)
+#endif
+static uint32_t kv_span(const KvLayer &c)
+{
+    if (c.tokens < 8u * (uint64_t)c.rows) return 1u;
+    return (uint64_t)c.tokens * c.kv_heads >= 32ull * QP_KV_SPAN_FILL ? 32u : 8u;
+}
 static dim3 kv_rows_grid(const KvLayer &c, uint32_t span)
 {
     const uint64_t waves = ((uint64_t)c.tokens + span - 1u) / span * c.kv_heads;

@@ -316,8 +316,9 @@ def test_the_books_against_one_row_after_the_other(qp, seed, rows, n_pages, per_
             seen |= {"short"} if short else {"out"} if out else {"copies"} if moves else set()
         elif op == "fork":
             parent = np.where((lengths == 0) | (rng.random(rows) < 0.05), rng.integers(-1, rows, rows), -1).astype(np.int32)
+            refused = int(pool[2])
             qp.qp_kv_fork(cache, r, pool, dev(parent))
-            assert int(pool[2]) == kp.fork(table, lengths, refs, parent, page)
+            assert int(pool[2]) - refused == kp.fork(table, lengths, refs, parent, page)
             moves = []
         elif op == "free":
             keep = np.where(rng.random(rows) < 0.5, rng.integers(0, 2, rows) * rng.integers(0, page * per_row, rows), -1).astype(np.int32)

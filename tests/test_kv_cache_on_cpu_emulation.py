@@ -307,7 +307,7 @@ def test_the_books_against_one_row_after_the_other(driver, tmp_path):
             for x, y in moves:
                 pages[:, y] = pages[:, x]
         elif op == "fork":
-            heads_of[2] = kp.fork(table, lengths, refs, a, page)
+            heads_of[2] += kp.fork(table, lengths, refs, a, page)
         else:
             kp.free(table, lengths, refs, a, page)
         for n in ("table", "lengths", "pool"):
