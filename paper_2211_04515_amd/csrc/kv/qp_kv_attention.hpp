@@ -216,7 +216,8 @@ template <bool MANY> struct AtParts {
 template <typename Count> __device__ __forceinline__ uint32_t at_share(uint64_t cost, uint64_t items, uint32_t slots, const Count &count)
 {
     const uint64_t goal = items <= slots ? slots : items <= 2u * slots ? 2u * slots : slots;
-    uint32_t per = (uint32_t)min(max((cost + goal - 1u) / goal, (uint64_t)kAtLeast), (uint64_t)0x3fffffffu);
+    const uint64_t share = cost + goal - 1u <= 0xffffffffull ? (uint32_t)(cost + goal - 1u) / (uint32_t)goal : (cost + goal - 1u) / goal;
+    uint32_t per = (uint32_t)min(max(share, (uint64_t)kAtLeast), (uint64_t)0x3fffffffu);
     if (items <= 2u * slots)
         for (int i = 0; i < 20 && count(per) > goal; ++i) per += max(1u, per / 16u);
     return per;
@@ -230,7 +231,9 @@ template <bool MANY> __device__ __forceinline__ bool at_find(const KvLayer &c, c
     none.tiles = 1u;
     if (c.rows <= (uint32_t)kWave) {             // every wave for itself, a row a lane: nothing to wait for but the lengths
         const AtRow o = lane < c.rows ? at_row<MANY>(c, a, w.wide, lane) : none;
-        const uint64_t cost = at_wave_sum((uint64_t)o.tiles * o.items) * c.kv_heads, items = (uint64_t)wave_sum_u32(o.items) * c.kv_heads;
+        const uint64_t steps = (uint64_t)o.tiles * o.items;
+        const uint64_t cost = (((uint64_t)wave_sum_u32((uint32_t)(steps >> 20)) << 20) + wave_sum_u32((uint32_t)steps & 0xfffffu)) * c.kv_heads;
+        const uint64_t items = (uint64_t)wave_sum_u32(o.items) * c.kv_heads;
         const uint32_t per = at_share(cost, items, w.slots, [&](uint32_t p) { return (uint64_t)wave_sum_u32(o.items * ((o.tiles + p - 1u) / p)) * c.kv_heads; });
         const AtParts<MANY> parts(c, o, per);
         uint32_t e[3] = {parts.blocks, parts.units, parts.cols};
@@ -1049,15 +1052,20 @@ template <int D, int DT> __global__ __launch_bounds__(kAtThreads) void k_kv_join
         const u32x4 rec = w.cols[k < first ? k : k - first];
         const uint32_t pieces = rec[1];
         if (pieces == 0u) continue;
-        float top = -3.402823466e38f;
-        for (uint32_t i = tid; i < pieces; i += kAtThreads) top = fmaxf(top, w.sums[rec[0] + (size_t)i * rec[2]].x);
+        // (a lane's first piece, and each wave's first row of numerators, on their way before the sums are known)
+        const float2 ml0 = tid < pieces ? w.sums[rec[0] + (size_t)tid * rec[2]] : float2{-3.402823466e38f, 0.0f};
+        float first_row[PER];
+#pragma unroll
+        for (int z = 0; z < PER; ++z) first_row[z] = wave < pieces && lane + kWave * z < (uint32_t)D ? w.nums[(rec[0] + (size_t)wave * rec[2]) * D + lane + kWave * z] : 0.0f;
+        float top = ml0.x;
+        for (uint32_t i = tid + kAtThreads; i < pieces; i += kAtThreads) top = fmaxf(top, w.sums[rec[0] + (size_t)i * rec[2]].x);
         top = wave_max(top);
         if (lane == 0u) top_of[wave] = top;
         __syncthreads();
         top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
         float sum = 0.0f;
         for (uint32_t i = tid; i < pieces; i += kAtThreads) {
-            const float2 ml = w.sums[rec[0] + (size_t)i * rec[2]];
+            const float2 ml = i == tid ? ml0 : w.sums[rec[0] + (size_t)i * rec[2]];
             const float e = at_exp2(ml.x - top);
             weight[i] = e;
             sum = fmaf(e, ml.y, sum);
@@ -1067,9 +1075,9 @@ template <int D, int DT> __global__ __launch_bounds__(kAtThreads) void k_kv_join
         __syncthreads();
         float acc[PER];
 #pragma unroll
-        for (int z = 0; z < PER; ++z) acc[z] = 0.0f;
+        for (int z = 0; z < PER; ++z) acc[z] = wave < pieces ? weight[wave] * first_row[z] : 0.0f;
 #pragma unroll 4
-        for (uint32_t i = wave; i < pieces; i += kAtWaves) {
+        for (uint32_t i = wave + kAtWaves; i < pieces; i += kAtWaves) {
             const float *src = w.nums + (rec[0] + (size_t)i * rec[2]) * D;
             const float e = weight[i];
 #pragma unroll

@@ -26,28 +26,44 @@ __device__ __forceinline__ int64_t kv_length(const qp_kv_rows_t &rows, uint32_t 
     return min(max((int64_t)rows.lengths_dev[r], (int64_t)0), cap);
 }
 
-// Inclusive prefix sum over the block's 1024 lanes; total: of all of them.  `part` holds one sum a wave.
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x)
+// Inclusive prefix sums of N numbers over the block's 1024 lanes, and their totals.  `part` holds each wave's.
+template <int N> __device__ __forceinline__ void wave_scan(uint32_t (&x)[N])
 {
     const uint32_t lane = threadIdx.x % kWave;
 #pragma unroll
-    for (uint32_t d = 1; d < (uint32_t)kWave; d *= 2u) {
-        const uint32_t o = __shfl_up(x, d, kWave);
-        if (lane >= d) x += o;
-    }
-    return x;
+    for (uint32_t d = 1; d < (uint32_t)kWave; d *= 2u)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t o = __shfl_up(x[i], d, kWave);
+            if (lane >= d) x[i] += o;
+        }
 }
-__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *part, uint32_t &total)
+template <int N> __device__ __forceinline__ void block_scan(uint32_t (&x)[N], uint32_t (*part)[kKvPlan / kWave], uint32_t (&total)[N])
 {
     const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const uint32_t x = wave_scan(v);
+    wave_scan(x);
     __syncthreads();                          // (the sums of an earlier scan have been read)
-    if (lane == kWave - 1u) part[wave] = x;
+    if (lane == kWave - 1u)
+#pragma unroll
+        for (int i = 0; i < N; ++i) part[i][wave] = x[i];
     __syncthreads();
-    const uint32_t sums = wave_scan(lane < (uint32_t)(kKvPlan / kWave) ? part[lane] : 0u);     // (every wave adds the 16 up for itself)
-    total = (uint32_t)__builtin_amdgcn_readlane((int)sums, kKvPlan / kWave - 1);
-    const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)sums, (int)(wave ? wave - 1u : 0u));
-    return x + (wave ? before : 0u);
+    uint32_t sums[N];                         // (every wave adds the 16 up for itself)
+#pragma unroll
+    for (int i = 0; i < N; ++i) sums[i] = lane < (uint32_t)(kKvPlan / kWave) ? part[i][lane] : 0u;
+    wave_scan(sums);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        total[i] = (uint32_t)__builtin_amdgcn_readlane((int)sums[i], kKvPlan / kWave - 1);
+        const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)sums[i], (int)(wave ? wave - 1u : 0u));
+        x[i] += wave ? before : 0u;
+    }
+}
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t (*part)[kKvPlan / kWave], uint32_t &total)
+{
+    uint32_t x[1] = {v}, t[1];
+    block_scan(x, part, t);
+    total = t[0];
+    return x[0];
 }
 
 __global__ __launch_bounds__(256) void k_kv_pool_init(int32_t *pool, uint32_t words)
@@ -119,7 +135,7 @@ __device__ __forceinline__ KvAsk kv_ask(const KvPages &c, const KvPool &p, uint3
 // that what it reads is read once: 15.5 -> RESERVE_US us for 40 rows.
 __global__ __launch_bounds__(kKvPlan) void k_kv_reserve(KvPages c, qp_kv_rows_t rows, const int32_t *__restrict__ want, void *pool)
 {
-    __shared__ uint32_t part[kKvPlan / kWave];
+    __shared__ uint32_t part[3][kKvPlan / kWave];
     __shared__ uint32_t ask_fresh[kKvPlan], ask_slot[kKvPlan], ask_base[kKvPlan];
     const uint32_t tid = threadIdx.x;
     const KvPool p = kv_pool(pool, c.n_pages);
@@ -150,11 +166,9 @@ __global__ __launch_bounds__(kKvPlan) void k_kv_reserve(KvPages c, qp_kv_rows_t 
         if (w.want > 0 && w.length + w.want > cap) ++over;
         else need += ask(r).fresh;
     }
-    uint32_t rows_over = 0, low = 0, high = 0;
-    block_scan(over, part, rows_over);
-    block_scan((uint32_t)need & 0xffffu, part, low);
-    block_scan((uint32_t)(need >> 16), part, high);
-    const uint32_t total = (uint32_t)min(((uint64_t)high << 16) + low, (uint64_t)0x7fffffffu);
+    uint32_t counts[3] = {over, (uint32_t)need & 0xffffu, (uint32_t)(need >> 16)}, sums[3];
+    block_scan(counts, part, sums);
+    const uint32_t rows_over = sums[0], total = (uint32_t)min(((uint64_t)sums[2] << 16) + sums[1], (uint64_t)0x7fffffffu);
     // the free pages with the lowest indices, as many as are needed
     uint32_t found = 0;
     for (uint32_t p0 = 0; p0 < c.n_pages && found < total && rows_over == 0u; p0 += kKvPlan * kKvScan) {
@@ -183,9 +197,9 @@ __global__ __launch_bounds__(kKvPlan) void k_kv_reserve(KvPages c, qp_kv_rows_t 
         const bool is = r < rows.rows;
         const KvWish w = is ? wish(r) : nothing;
         const KvAsk a = is ? ask(r) : none;
-        uint32_t sum = 0, copies = 0;
-        const uint32_t mine = base + block_scan(a.fresh, part, sum) - a.fresh;
-        const uint32_t move = moves + block_scan(a.copy ? 1u : 0u, part, copies) - (a.copy ? 1u : 0u);
+        uint32_t at[2] = {a.fresh, a.copy ? 1u : 0u}, all[2];
+        block_scan(at, part, all);
+        const uint32_t mine = base + at[0] - a.fresh, move = moves + at[1] - (a.copy ? 1u : 0u);
         ask_fresh[tid] = a.fresh;
         ask_slot[tid] = a.slot;
         ask_base[tid] = mine;
@@ -198,8 +212,8 @@ __global__ __launch_bounds__(kKvPlan) void k_kv_reserve(KvPages c, qp_kv_rows_t 
         for (uint32_t k = tid / kWave; k < min((uint32_t)kKvPlan, rows.rows - r0); k += kKvPlan / kWave)   // a wave a row: its pages
             for (uint32_t i = tid % kWave; i < ask_fresh[k]; i += kWave)
                 rows.table_dev[(uint64_t)(r0 + k) * rows.pages_per_row + ask_slot[k] + i] = p.list[ask_base[k] + i];
-        base += sum;
-        moves += copies;
+        base += all[0];
+        moves += all[1];
         __syncthreads();
     }
     // the counts change once no row looks at them any more; the shared pages' books are cleared for the next call
@@ -268,7 +282,7 @@ __global__ __launch_bounds__(256) void k_kv_free(KvPages c, qp_kv_rows_t rows, c
 // of the one as of the other.  `count` (all zero between calls) says where a moved page went, + 1.
 __global__ __launch_bounds__(kKvPlan) void k_kv_compact(KvPages c, void *pool)
 {
-    __shared__ uint32_t part[kKvPlan / kWave];
+    __shared__ uint32_t part[3][kKvPlan / kWave];
     const uint32_t tid = threadIdx.x;
     const KvPool p = kv_pool(pool, c.n_pages);
     uint32_t live = 0, mine = 0;
@@ -291,16 +305,16 @@ __global__ __launch_bounds__(kKvPlan) void k_kv_compact(KvPages c, void *pool)
             below += is && at + i < live ? 1u : 0u;
             above += is && at + i >= live ? 1u : 0u;
         }
-        uint32_t h = 0, m = 0;
-        uint32_t hole = holes + block_scan(below, part, h) - below;
-        uint32_t mover = movers + block_scan(above, part, m) - above;
+        uint32_t at2[2] = {below, above}, all[2];
+        block_scan(at2, part, all);
+        uint32_t hole = holes + at2[0] - below, mover = movers + at2[1] - above;
         for (uint32_t i = 0; i < (uint32_t)kKvScan; ++i)
             if ((bits >> i) & 1u) {
                 if (at + i < live) p.pairs[2u * hole++ + 1u] = (int32_t)(at + i);
                 else p.pairs[2u * mover++] = (int32_t)(at + i);
             }
-        holes += h;
-        movers += m;
+        holes += all[0];
+        movers += all[1];
     }
     __syncthreads();                          // the pairs are whole
     for (uint32_t i = tid; i < holes; i += kKvPlan) {
