@@ -498,10 +498,10 @@ template <int D, int NCT, int DT> struct AtWave {
             float x = fmaxf(top[t], kv_xor_f32(top[t], 16));
             x = fmaxf(x, kv_xor_f32(x, 32));
             const bool first = over[t] < 0.0f;
-            const float up = x == -INFINITY ? 0.0f : first ? x : fmaxf(x, 0.0f);     // (x NaN: 0 or NaN; the column is lost anyway)
+            const float next = x == -INFINITY ? m[t] : m[t] + (first ? x : fmaxf(x, 0.0f)), up = next - m[t];   // (what m moves by once rounded)
             over[t] = x == -INFINITY ? over[t] : kAtHeadroom;
             const float alpha = first ? 1.0f : at_exp2(-up);                          // (first: there is nothing to scale)
-            m[t] += up;
+            m[t] = next;
             l[t] *= alpha;
             lv[t] *= alpha;
             const float beta = alpha * ratio;
@@ -618,7 +618,12 @@ template <int D, int NCT, int DT> struct AtWave {
                     const float e = at_exp2(x.s[u][t][i / 4][i % 4]);
                     l[t] += e;
                     lv[t] = fmaf(e, bv[i], lv[t]);
-                    const float w = e * sv[i];
+                    float w = e * sv[i];
+#if defined(__AMDGCN__)
+                    // (else one half's product is rounded to fp32 first and the other's is not, and where that makes a difference, once in
+                    // 2^13 weights, the halves do not add up: answers off by 1e-4)
+                    if constexpr (PIECES == 2) asm volatile("" : "+v"(w));
+#endif
                     const int at = i % 4 * 2 + i / 4;     // code order
                     p[t][0][at] = (_Float16)w;
                     if constexpr (PIECES == 2) p[t][1][at] = (_Float16)(w - (float)p[t][0][at]);
@@ -629,15 +634,8 @@ template <int D, int NCT, int DT> struct AtWave {
                 const f16x8 a = value(u, b);
 #pragma unroll
                 for (int t = 0; t < NCT; ++t)
-                    if constexpr (PIECES == 1) {
-                        o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][0], o[t][b], 0, 0, 0);
-                    } else {
-                        // added up outside the matrix unit: its sums of the whole row drift by a few 2^-18 (measured 3e-6 of the answer at
-                        // 1000 tokens; so 7e-7, the plain fp32 form's error)
-                        const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-                        const f32x4 part = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][1], zero, 0, 0, 0);
-                        o[t][b] += __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][0], part, 0, 0, 0);
-                    }
+#pragma unroll
+                    for (int z = PIECES - 1; z >= 0; --z) o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[t][z], o[t][b], 0, 0, 0);
             }
         }
     }

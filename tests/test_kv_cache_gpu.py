@@ -229,6 +229,20 @@ def test_the_same_on_every_run_and_stream(qp):
     assert torch.equal(other, first)
 
 
+@pytest.mark.parametrize("dim,group,lengths,counts", [(128, 1, [1024] * 8, [1] * 8), (80, 4, [2000] * 4, [1] * 4), (64, 2, [600, 900], [200, 60])])
+def test_fp32_answers_are_fp32(qp, dim, group, lengths, counts):
+    """The 2-norm over all answers, where a single weight that lost its lower half (2^-12 of it) shows: the roundings of one answer are
+    independent of each other, so that they add up like the square root of their number, at most dim + 2 log2(n) + 32 < 256 of 2^-24 B
+    with B, the terms' size over the answer's, below 16 here: 16 sqrt(256) 2^-24 = 2^-16 of each answer."""
+    c = Case(qp, dim, 64, 2, lengths)
+    q = c.rng.standard_normal((sum(counts), 2 * group, dim)).astype(np.float32)
+    o = c.attend(counts, group, "f32", q=q).double().cpu().numpy()
+    begin = np.concatenate([[0], np.cumsum(counts)])
+    want, _ = kp.attention(c.pages[0], dim, 64, c.table, c.lengths, begin, q, float(np.float32(dim ** -0.5)), True, 0, 2.0 ** -24, True)
+    per = np.linalg.norm(o - want, axis=-1) / np.linalg.norm(want, axis=-1)
+    assert per.max() <= 2.0 ** -16, per.max()
+
+
 # ---- rows in and out ---------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
