@@ -413,7 +413,8 @@ qp_status qp_controller_update(qp_controller_t *c, double payload_bits, double s
  * Tokens of a call.  token_begin_dev[0 .. rows] says which of the `tokens` tokens of the call's tensors belong to which row:
  * row r has tokens token_begin_dev[r] .. token_begin_dev[r + 1] - 1 (ascending; cut off at 0 and `tokens`).  For qp_kv_append and
  * qp_kv_attention they are the row's LAST tokens: lengths_dev counts them already, as qp_kv_reserve leaves it.  (Should a row
- * have more of them than its length, the first ones have no place: they are not stored, and see nothing.)
+ * have more of them than its length, the first ones have no place: they are not stored, and see nothing.)  Tokens that are no row's
+ * are left alone: not stored, and their place in an output stays as it was.  tokens and tokens * heads are below 2^31.
  *
  * A step of a serving loop is qp_kv_reserve once, then qp_kv_append and qp_kv_attention for each layer.  All calls are
  * asynchronous on `stream` and may be captured into a graph; results do not depend on the order of atomics.  Calls that touch
@@ -449,7 +450,7 @@ typedef struct {
 size_t qp_kv_page_bytes(const qp_kv_cache_t *cache);
 
 /* ---- pages: handing out, sharing, freeing, moving together -----------------------------
- * The pool record is int32 words in device memory: QP_KV_POOL_HEADER of header, then refs[n_pages], how many rows hold each page
+ * The pool record is int32 words in device memory, 4-byte aligned: QP_KV_POOL_HEADER of header, then refs[n_pages], how many rows hold each page
  * (0 = free), then room that the calls work in.  Header word 0: pages that the last qp_kv_reserve was short of (0: it was done);
  * word 1: rows of the last qp_kv_reserve that would have outgrown pages_per_row; word 2: rows that qp_kv_fork has refused so
  * far (it only adds; the caller may clear it); word 3: pages in use after the last qp_kv_compact.  qp_kv_pool_init makes every page free (do it once; it also clears
@@ -491,9 +492,11 @@ qp_status qp_kv_read(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, uint3
  * out = softmax(scale * q K^T) V for each of the call's tokens and each of q_heads query heads; query head h goes with key head
  * h div (q_heads / kv_heads).  causal: token i of a row's m, at position p = length - m + i, sees tokens t <= p, and with window > 0
  * only t > p - window; without causal it sees the whole row (window must be 0).  A query that sees nothing gives 0; one
- * that holds NaN or Inf gives NaN, and no other query does.  Dot products of codes and queries are exact, sums and softmax are fp32;
- * out has q's type.  Long rows are split among blocks and joined in a fixed order: results are the same on every run.
- * The workspace needs no initialisation. */
+ * that holds NaN or Inf gives NaN, and no other query does.  Products take the codes as they are (no value is rounded), bf16
+ * queries too (elements below 2^-14 to 2^-29), fp32 queries to 22 bits and weights to 11 (bf16) or 22 (fp32); scores, maxima, sums and
+ * numerators are fp32; out has q's type.  Long rows are split among blocks and joined in a fixed order: results are the same on
+ * every run.  out may be q itself (the same strides); otherwise it overlaps neither q nor the cache.  The workspace needs no
+ * initialisation; calls that may run at the same time (two streams, two graphs) need one each. */
 typedef struct {
     float    scale;            /* > 0, finite */
     uint32_t q_heads;          /* a multiple of kv_heads, at most 1024 times it */

@@ -470,6 +470,13 @@ def _kv_call(device, stream, what: str, *args) -> None:
     _check(st, what)
 
 
+def _uint(v: int, what: str) -> int:
+    """A number for a 32-bit field, which ctypes would cut down to its low bits."""
+    if not 0 <= int(v) < 1 << 32:
+        raise QuantPipeError(QP_EINVAL, what)
+    return int(v)
+
+
 def qp_kv_page_bytes(cache: qp_kv_cache_t) -> int:
     return int(lib().qp_kv_page_bytes(C.byref(cache)))
 
@@ -525,7 +532,7 @@ def qp_kv_append(cache, rows, layer: int, token_begin, k, v, stream=None) -> Non
     _same_device(d, rows)
     n = k.shape[0]
     kv, vv = _view(k, cache.kv_heads, cache.head_dim, n, d), _view(v, cache.kv_heads, cache.head_dim, n, d)
-    _kv_call(d, stream, "qp_kv_append", C.byref(cache), C.byref(rows), int(layer), _ints(token_begin, rows.rows + 1, d), n, C.byref(kv), C.byref(vv))
+    _kv_call(d, stream, "qp_kv_append", C.byref(cache), C.byref(rows), _uint(layer, "qp_kv_append"), _ints(token_begin, rows.rows + 1, d), n, C.byref(kv), C.byref(vv))
 
 
 def qp_kv_read(cache, rows, layer: int, token_begin, k, v, first=None, stream=None) -> None:
@@ -535,7 +542,7 @@ def qp_kv_read(cache, rows, layer: int, token_begin, k, v, first=None, stream=No
     n = k.shape[0]
     kv, vv = _view(k, cache.kv_heads, cache.head_dim, n, d), _view(v, cache.kv_heads, cache.head_dim, n, d)
     f = None if first is None else _ints(first, rows.rows, d)
-    _kv_call(d, stream, "qp_kv_read", C.byref(cache), C.byref(rows), int(layer), _ints(token_begin, rows.rows + 1, d), f, n, C.byref(kv), C.byref(vv))
+    _kv_call(d, stream, "qp_kv_read", C.byref(cache), C.byref(rows), _uint(layer, "qp_kv_read"), _ints(token_begin, rows.rows + 1, d), f, n, C.byref(kv), C.byref(vv))
 
 
 def qp_kv_attention(cache, rows, layer: int, token_begin, q, out, ws, scale: float = None, causal: bool = True, window: int = 0,
@@ -547,6 +554,6 @@ def qp_kv_attention(cache, rows, layer: int, token_begin, q, out, ws, scale: flo
     qv, ov = _view(q, heads, cache.head_dim, n, d), _view(out, heads, cache.head_dim, n, d)
     if ws.device != d or not ws.is_contiguous():
         raise ValueError("expected a contiguous workspace on %s" % d)
-    cfg = qp_kv_attn_cfg_t(cache.head_dim ** -0.5 if scale is None else scale, heads, 1 if causal else 0, int(window))
-    _kv_call(d, stream, "qp_kv_attention", C.byref(cache), C.byref(rows), int(layer), _ints(token_begin, rows.rows + 1, d), n, C.byref(qv), C.byref(ov),
+    cfg = qp_kv_attn_cfg_t(cache.head_dim ** -0.5 if scale is None else scale, heads, 1 if causal else 0, _uint(window, "qp_kv_attention"))
+    _kv_call(d, stream, "qp_kv_attention", C.byref(cache), C.byref(rows), _uint(layer, "qp_kv_attention"), _ints(token_begin, rows.rows + 1, d), n, C.byref(qv), C.byref(ov),
              C.byref(cfg), ws.data_ptr(), ws.numel() * ws.element_size())

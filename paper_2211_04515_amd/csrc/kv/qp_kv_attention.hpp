@@ -780,20 +780,8 @@ __device__ __forceinline__ void at_store(const AtWave<D, NCT, DT> &x, const AtBl
     }
 }
 
-#ifndef QP_KV_FEW_WAVES
-#define QP_KV_FEW_WAVES 2
-#endif
-#ifndef QP_AHEAD
-#define QP_AHEAD 2
-#endif
-#ifndef QP_SUB
-#define QP_SUB 2
-#endif
-#ifndef QP_KV_MANY_WAVES
-#define QP_KV_MANY_WAVES 2
-#endif
 template <int D, int DT>
-__global__ __launch_bounds__(kAtThreads, D <= 128 ? QP_KV_FEW_WAVES : 1) void k_kv_attention_few(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
+__global__ __launch_bounds__(kAtThreads, D <= 128 ? 2 : 1) void k_kv_attention_few(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
 {
     using Wave = AtWave<D, 1, DT>;
     constexpr int NB = Wave::NB;
@@ -810,8 +798,9 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 ? QP_KV_FEW_WAVES : 1) void k_
         there = page >= 0;
         return kv_slab(c, there ? page : 0, b.p.head);
     };
-    // Three steps' words: those of a step are fetched again, for the one after the next two, as soon as it is done with them.
-    constexpr int kAhead = QP_AHEAD;
+    // Two steps' words are on their way: a step's registers are filled again, for the step after the next, as soon as it is done
+    // with them.  (Three or four fit no longer three blocks on a CU.)
+    constexpr int kAhead = 2;
     Wave x;
     typename Wave::Query query;
     typename Wave::Raw raw[kAhead];
@@ -875,13 +864,13 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 ? QP_KV_FEW_WAVES : 1) void k_
 }
 
 template <int D, int DT>
-__global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? QP_KV_MANY_WAVES : 1) void k_kv_attention_many(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
+__global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? 2 : 1) void k_kv_attention_many(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
 {
     constexpr int NCT = 2;
     using Wave = AtWave<D, NCT, DT>;
     constexpr int NB = Wave::NB, KS = Wave::KS;
     constexpr uint32_t kFrags = 2 * KS + NB;                        // fragments of 32 tokens: keys (j, k), then values
-    constexpr uint32_t kSub = D <= 128 ? QP_SUB : 1, kStage = kSub * kAtStep;      // tokens between two barriers
+    constexpr uint32_t kSub = D <= 128 ? 2 : 1, kStage = kSub * kAtStep;      // tokens between two barriers
     struct Stage {
         f16x8 frags[kFrags][kWave];
         float2 grids[64];

@@ -229,6 +229,72 @@ def test_the_same_on_every_run_and_stream(qp):
     assert torch.equal(other, first)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_heads_share_a_key_head_than_a_block_has_columns(qp, dtype):
+    Case(qp, 64, 32, 1, [300, 5]).attend([1, 2], 200, dtype)
+    Case(qp, 64, 32, 1, [700]).attend([1], 1024, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lengths,counts", [([4000, 30], [1, 3]), ([1500, 300], [260, 1])])
+def test_the_answer_may_take_the_query_s_place(qp, lengths, counts, dtype):
+    c = Case(qp, 128, 64, 2, lengths)
+    q = torch.from_numpy(c.rng.standard_normal((sum(counts), 8, 128))).to(TYPES[dtype]).cuda()
+    begin = dev(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32))
+    ws = qp.alloc_kv_workspace(c.cache, c.rows, sum(counts), 8)
+    out = torch.empty_like(q)
+    qp.qp_kv_attention(c.cache, c.rows, 0, begin, q, out, ws)
+    qp.qp_kv_attention(c.cache, c.rows, 0, begin, q, q, ws)
+    assert torch.equal(q, out)
+
+
+def test_calls_and_graphs_at_once_with_a_workspace_each(qp):
+    """Two streams, then two graphs on two streams, over one cache: each its own answers, replay after replay."""
+    c = Case(qp, 128, 64, 4, [5000, 300, 2222])
+    g = torch.Generator("cuda").manual_seed(6)
+    jobs = []
+    for counts in ([1, 1, 1], [90, 1, 40]):
+        n = sum(counts)
+        j = dict(q=torch.randn(n, 16, 128, device="cuda", generator=g).bfloat16(), begin=dev(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)),
+                 ws=qp.alloc_kv_workspace(c.cache, c.rows, n, 16), stream=torch.cuda.Stream())
+        j["out"], j["want"] = torch.empty_like(j["q"]), torch.empty_like(j["q"])
+        qp.qp_kv_attention(c.cache, c.rows, 0, j["begin"], j["q"], j["want"], j["ws"])
+        jobs.append(j)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for j in jobs:
+            qp.qp_kv_attention(c.cache, c.rows, 0, j["begin"], j["q"], j["out"], j["ws"], stream=j["stream"])
+    torch.cuda.synchronize()
+    assert all(torch.equal(j["out"], j["want"]) for j in jobs)
+    for j in jobs:
+        j["graph"] = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(j["graph"]):
+            for _ in range(3):
+                qp.qp_kv_attention(c.cache, c.rows, 0, j["begin"], j["q"], j["out"], j["ws"])
+    for _ in range(4):
+        for j in jobs:
+            j["out"].zero_()
+        torch.cuda.synchronize()
+        for j in jobs:
+            with torch.cuda.stream(j["stream"]):
+                j["graph"].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(j["out"], j["want"]) for j in jobs)
+
+
+def test_numbers_past_32_bits_are_refused(qp):
+    c = Case(qp, 64, 32, 1, [40])
+    q = torch.ones(1, 1, 64, device="cuda")
+    ws = qp.alloc_kv_workspace(c.cache, c.rows, 1, 1)
+    for layer, window in ((2 ** 32, 0), (-1, 0), (0, 2 ** 32), (0, 2 ** 31), (0, -1)):
+        with pytest.raises(qp.QuantPipeError):
+            qp.qp_kv_attention(c.cache, c.rows, layer, ints(0, 1), q, q, ws, window=window)
+    for call in (qp.qp_kv_append, qp.qp_kv_read):
+        with pytest.raises(qp.QuantPipeError):
+            call(c.cache, c.rows, 2 ** 32, ints(0, 1), q, q)
+    assert (q == 1).all()
+
+
 @pytest.mark.parametrize("dim,group,lengths,counts", [(128, 1, [1024] * 8, [1] * 8), (80, 4, [2000] * 4, [1] * 4), (64, 2, [600, 900], [200, 60])])
 def test_fp32_answers_are_fp32(qp, dim, group, lengths, counts):
     """The 2-norm over all answers, where a single weight that lost its lower half (2^-12 of it) shows: the roundings of one answer are
