@@ -64,6 +64,19 @@ __host__ __device__ inline KvPool kv_pool(void *pool, uint32_t n_pages)
 }
 enum : uint32_t { kKvShort = 0, kKvOutgrown = 1, kKvRefused = 2, kKvLive = 3, kKvMoves = 4 };   // words of the header
 
+// Inclusive prefix sums over a wave's lanes: within rows of 16 by shifts that bring in zeros, then what the rows before come to.
+__device__ __forceinline__ uint32_t kv_wave_scan(uint32_t v)
+{
+    int x = (int)v;
+    x += dpp_i32<0x111>(x);                     // row_shr:1, 2, 4, 8
+    x += dpp_i32<0x112>(x);
+    x += dpp_i32<0x114>(x);
+    x += dpp_i32<0x118>(x);
+    const uint32_t row = threadIdx.x % kWave / 16u;
+    const int a = __builtin_amdgcn_readlane(x, 15), b = a + __builtin_amdgcn_readlane(x, 31), c = b + __builtin_amdgcn_readlane(x, 47);
+    return (uint32_t)(x + (row == 0u ? 0 : row == 1u ? a : row == 2u ? b : c));
+}
+
 hipError_t launch_kv_append(const KvLayer &c, uint32_t dim, int dtype, const KvView &k, const KvView &v, hipStream_t s);
 hipError_t launch_kv_read(const KvLayer &c, uint32_t dim, int dtype, const int32_t *first, const KvView &k, const KvView &v,
                           hipStream_t s);

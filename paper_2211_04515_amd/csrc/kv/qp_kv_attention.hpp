@@ -151,12 +151,7 @@ __device__ __forceinline__ void at_scan(uint32_t (&x)[3], uint32_t (*part)[3], u
 {
     const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
 #pragma unroll
-    for (uint32_t d = 1; d < (uint32_t)kWave; d *= 2u)
-#pragma unroll
-        for (int i = 0; i < 3; ++i) {
-            const uint32_t o = __shfl_up(x[i], d, kWave);
-            if (lane >= d) x[i] += o;
-        }
+    for (int i = 0; i < 3; ++i) x[i] = kv_wave_scan(x[i]);
     if (lane == kWave - 1u)
 #pragma unroll
         for (int i = 0; i < 3; ++i) part[wave][i] = x[i];
@@ -241,14 +236,7 @@ template <bool MANY> __device__ __forceinline__ bool at_find(const KvLayer &c, c
         const uint64_t items = (uint64_t)wave_sum_u32(o.items) * c.kv_heads;
         const uint32_t per = at_share(cost, items, w.slots, [&](uint32_t p) { return (uint64_t)wave_sum_u32(o.items * ((o.tiles + p - 1u) / p)) * c.kv_heads; });
         const AtParts<MANY> parts(c, o, per);
-        uint32_t e[3] = {parts.blocks, parts.units, parts.cols};
-#pragma unroll
-        for (uint32_t d = 1; d < (uint32_t)kWave; d *= 2u)
-#pragma unroll
-            for (int i = 0; i < 3; ++i) {
-                const uint32_t x = __shfl_up(e[i], d, kWave);
-                if (lane >= d) e[i] += x;
-            }
+        const uint32_t e[3] = {kv_wave_scan(parts.blocks), kv_wave_scan(parts.units), kv_wave_scan(parts.cols)};
         const bool fits = parts.fits(w, e);
         if (block == 0u && tid < (uint32_t)kWave) {
             const uint32_t split = wave_max_u32(fits && parts.cols != 0u ? e[2] : 0u);

@@ -6,8 +6,8 @@
 // pool (the lowest free page first), which one block of 1024 lanes keeps with prefix sums: it reads 32 KB of reference counts at a
 // time.  Sharing and giving up only add to counts, whose order does not matter.
 // The copy kernel is bound by HBM: 16-byte loads and stores, all layers' pages of a list spread over the whole chip.  Measured: 117 us where
-// 16 layers' pages of 48 requests move together, 127 with the books before it, 5.2 TB/s read and written; a large plain copy runs at 4.7.
-// A beam step (8 requests of 5 beams: free, fork, reserve, 32 pages of 16 layers copied) is 31 us: 16.5 of copying (4.6 TB/s), 9.8 to reserve,
+// 16 layers' pages of 48 requests move together (232 of 1.2 MB), 126 with the books before it, 4.7 TB/s read and written, a large plain copy's rate.
+// A beam step (8 requests of 5 beams: free, fork, reserve, 32 pages of 16 layers copied) is 29 us: 16.4 of copying (4.6 TB/s), 7.8 to reserve,
 // 3.5 to fork, 2.8 to free.
 #include "qp_kv.hpp"
 
@@ -32,14 +32,8 @@ __device__ __forceinline__ int64_t kv_length(const qp_kv_rows_t &rows, uint32_t 
 // Inclusive prefix sums of N numbers over the block's 1024 lanes, and their totals.  `part` holds each wave's.
 template <int N> __device__ __forceinline__ void wave_scan(uint32_t (&x)[N])
 {
-    const uint32_t lane = threadIdx.x % kWave;
 #pragma unroll
-    for (uint32_t d = 1; d < (uint32_t)kWave; d *= 2u)
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint32_t o = __shfl_up(x[i], d, kWave);
-            if (lane >= d) x[i] += o;
-        }
+    for (int i = 0; i < N; ++i) x[i] = kv_wave_scan(x[i]);
 }
 template <int N> __device__ __forceinline__ void block_scan(uint32_t (&x)[N], uint32_t (*part)[kKvPlan / kWave], uint32_t (&total)[N])
 {
@@ -135,11 +129,12 @@ __device__ __forceinline__ KvAsk kv_ask(const KvPages &c, const KvPool &p, uint3
 }
 
 // Latency is all that it costs: a lane keeps its first row's wish and ask in registers (most calls have no more rows than lanes), so
-// that what it reads is read once: 15.5 -> 9.8 us for 40 rows.
+// that what it reads is read once: 15.5 -> 9.8 us for 40 rows; the list of new pages in LDS 9.1, sums by lane shifts instead of LDS 7.8.
 __global__ __launch_bounds__(kKvPlan) void k_kv_reserve(KvPages c, qp_kv_rows_t rows, const int32_t *__restrict__ want, void *pool)
 {
     __shared__ uint32_t part[3][kKvPlan / kWave];
     __shared__ uint32_t ask_fresh[kKvPlan], ask_slot[kKvPlan], ask_base[kKvPlan];
+    __shared__ int32_t near_list[kKvPlan];    // the first of the new pages; what does not fit goes to the pool's room
     const uint32_t tid = threadIdx.x;
     const KvPool p = kv_pool(pool, c.n_pages);
     const KvWish nothing{0, 0, -1};
@@ -187,14 +182,16 @@ __global__ __launch_bounds__(kKvPlan) void k_kv_reserve(KvPages c, qp_kv_rows_t 
         uint32_t place = found + block_scan(mine, part, sum) - mine;
         for (uint32_t i = 0; i < (uint32_t)kKvScan; ++i)
             if ((bits >> i) & 1u) {
-                if (place < total) p.list[place] = (int32_t)(at + i);
+                if (place < min(total, (uint32_t)kKvPlan)) near_list[place] = (int32_t)(at + i);
+                else if (place < total) p.list[place] = (int32_t)(at + i);
                 ++place;
             }
         found += sum;
     }
     const bool done = rows_over == 0u && found >= total;
+    const auto page_at = [&](uint32_t k) { return k < (uint32_t)kKvPlan ? near_list[k] : p.list[k]; };
     __syncthreads();                          // the list is whole
-    uint32_t base = 0, moves = 0;
+    uint32_t base = 0, moves = 0, first_moves = 0;
     for (uint32_t r0 = 0; r0 < rows.rows && done; r0 += kKvPlan) {
         const uint32_t r = r0 + tid;
         const bool is = r < rows.rows;
@@ -208,23 +205,28 @@ __global__ __launch_bounds__(kKvPlan) void k_kv_reserve(KvPages c, qp_kv_rows_t 
         ask_base[tid] = mine;
         if (a.copy) {
             p.pairs[2u * move] = w.shared;
-            p.pairs[2u * move + 1u] = p.list[mine];
+            p.pairs[2u * move + 1u] = page_at(mine);
         }
         __syncthreads();                      // every row of these has looked at the counts and the table
         if (is && w.want > 0) rows.lengths_dev[r] = (int32_t)(w.length + w.want);
         for (uint32_t k = tid / kWave; k < min((uint32_t)kKvPlan, rows.rows - r0); k += kKvPlan / kWave)   // a wave a row: its pages
             for (uint32_t i = tid % kWave; i < ask_fresh[k]; i += kWave)
-                rows.table_dev[(uint64_t)(r0 + k) * rows.pages_per_row + ask_slot[k] + i] = p.list[ask_base[k] + i];
+                rows.table_dev[(uint64_t)(r0 + k) * rows.pages_per_row + ask_slot[k] + i] = page_at(ask_base[k] + i);
         base += all[0];
         moves += all[1];
+        if (r0 == 0u) first_moves = moves;
         __syncthreads();
     }
     // the counts change once no row looks at them any more; the shared pages' books are cleared for the next call
     if (done) {
-        for (uint32_t i = tid; i < total; i += kKvPlan) p.refs[p.list[i]] = 1;
-        for (uint32_t i = tid; i < moves; i += kKvPlan) atomicAdd(reinterpret_cast<uint32_t *>(p.refs + p.pairs[2u * i]), 0xffffffffu);
+        for (uint32_t i = tid; i < total; i += kKvPlan) p.refs[page_at(i)] = 1;
+        if (first_ask.copy) atomicAdd(reinterpret_cast<uint32_t *>(p.refs + first.shared), 0xffffffffu);
+        for (uint32_t i = first_moves + tid; i < moves; i += kKvPlan) {          // (of rows behind the first 1024)
+            const int32_t page = p.pairs[2u * i];
+            atomicAdd(reinterpret_cast<uint32_t *>(p.refs + page), 0xffffffffu);
+            p.count[page] = p.last[page] = 0;
+        }
     }
-    for (uint32_t i = tid; i < moves; i += kKvPlan) p.count[p.pairs[2u * i]] = p.last[p.pairs[2u * i]] = 0;
     if (tid < rows.rows && first.shared >= 0) p.count[first.shared] = p.last[first.shared] = 0;
     for (uint32_t r = tid + kKvPlan; r < rows.rows; r += kKvPlan) {   // (a counted page that was not copied is still its row's next one)
         const int64_t len = kv_length(rows, r, c.page_shift) - (done && want[r] > 0 ? want[r] : 0);

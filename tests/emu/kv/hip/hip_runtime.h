@@ -28,6 +28,16 @@ inline f4 mfma_16x16x32(h8 a, h8 b, f4 c)
     return c;
 }
 }  // namespace emu
+// shifts within rows of 16 lanes that bring in zeros; the other permutations are the common header's
+static inline int emu_kv_dpp(uint32_t v, int ctrl)
+{
+    if (ctrl < 0x111 || ctrl > 0x11f) return (int)emu::exchange(v, -1, ctrl, 0);
+    const unsigned lane = threadIdx.x % 64, by = (unsigned)ctrl & 15u, from = lane % 16 < by ? lane : lane - by;
+    const uint32_t o = emu::exchange(v, (int)from, -1, 0);
+    return lane % 16 < by ? 0 : (int)o;
+}
+#undef __builtin_amdgcn_update_dpp
+#define __builtin_amdgcn_update_dpp(old, v, ctrl, rm, bm, bc) emu_kv_dpp((uint32_t)(v), (ctrl))
 #define __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, x, y, z) emu::mfma_16x16x32((a), (b), (c))
 #define __builtin_amdgcn_wave_barrier() emu::wave_barrier()
 #define __builtin_amdgcn_exp2f(x) exp2f(x)
