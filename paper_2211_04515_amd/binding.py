@@ -406,7 +406,7 @@ def kv_cache(pages, kv_heads: int, head_dim: int, page_tokens: int) -> qp_kv_cac
     c = qp_kv_cache_t(pages.data_ptr(), pages.numel(), pages.shape[0], pages.shape[1], kv_heads, head_dim, page_tokens, 0)
     if qp_kv_page_bytes(c) == 0:
         raise QuantPipeError(QP_EINVAL, "kv_cache")
-    c.tensors = (pages,)
+    c.tensors, c.device = (pages,), pages.get_device()
     return c
 
 
@@ -414,8 +414,9 @@ def kv_rows(table, lengths) -> qp_kv_rows_t:
     """Rows with their page table, int32 [rows, pages_per_row], and lengths, int32 [rows]."""
     if table.dim() != 2 or tuple(lengths.shape) != (table.shape[0],):
         raise ValueError("expected table [rows, pages_per_row] and lengths [rows]")
-    r = qp_kv_rows_t(_ints(table, table.numel(), table.device), _ints(lengths, table.shape[0], table.device), table.shape[0], table.shape[1])
-    r.tensors = (table, lengths)
+    device = table.get_device()
+    r = qp_kv_rows_t(_ints(table, 0, device), _ints(lengths, 0, device), *table.shape)
+    r.tensors, r.device = (table, lengths), device
     return r
 
 
@@ -444,30 +445,34 @@ def alloc_kv_workspace(cache: qp_kv_cache_t, rows: qp_kv_rows_t, tokens: int, q_
     return torch.empty(nb, dtype=torch.uint8, device=cache.tensors[0].device)
 
 
-def _ints(t, count: int, device):
-    if t.dtype != torch.int32 or t.numel() < count or not t.is_contiguous() or not t.is_cuda or t.device != device:
-        raise ValueError("expected a contiguous int32 tensor of at least %d entries on %s" % (count, device))
+# (A call's checks in Python are what the smallest calls cost: devices are compared as numbers, -1 is none, and a tensor's shape is asked for once.)
+def _ints(t, count: int, device: int) -> int:
+    if t.dtype != torch.int32 or t.numel() < count or not t.is_contiguous() or t.get_device() != device or device < 0:
+        raise ValueError("expected a contiguous int32 tensor of at least %d entries on device %d" % (count, device))
     return t.data_ptr()
 
 
-def _view(t, heads: int, dim: int, tokens: int, device) -> qp_kv_view_t:
-    if t.dim() != 3 or t.shape[0] != tokens or t.shape[1] != heads or t.shape[2] != dim or t.device != device:
-        raise ValueError("expected a tensor [%d, %d, %d] on %s, got %s on %s" % (tokens, heads, dim, device, tuple(t.shape), t.device))
-    s = t.stride()
-    if s[2] != 1:
+def _view(t, heads: int, dim: int, tokens: int, device: int) -> qp_kv_view_t:
+    if t.shape != (tokens, heads, dim) or t.get_device() != device:
+        raise ValueError("expected a tensor [%d, %d, %d] on device %d, got %s on %s" % (tokens, heads, dim, device, tuple(t.shape), t.device))
+    a, b, c = t.stride()
+    if c != 1:
         raise ValueError("the elements of a head must lie next to each other")
     # (an axis of one entry may carry any stride: it is never used)
-    return qp_kv_view_t(t.data_ptr(), dtype_of(t), 0, s[0] if tokens > 1 else 0, s[1] if heads > 1 else 0)
+    return qp_kv_view_t(t.data_ptr(), dtype_of(t), 0, a if tokens > 1 else 0, b if heads > 1 else 0)
 
 
-def _kv_call(device, stream, what: str, *args) -> None:
+def _kv_call(device: int, stream, what: str, *args) -> None:
     """The library's call on the device's own current stream, with that device current (kernels go to the current one)."""
-    if device.index == torch.cuda.current_device():
-        st = getattr(lib(), what)(*args, C.c_void_p((torch.cuda.current_stream() if stream is None else stream).cuda_stream))
+    call = getattr(lib(), what)
+    handle = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    if device == torch.cuda.current_device():
+        st = call(*args, handle)
     else:
         with torch.cuda.device(device):
-            st = getattr(lib(), what)(*args, C.c_void_p((torch.cuda.current_stream() if stream is None else stream).cuda_stream))
-    _check(st, what)
+            st = call(*args, handle)
+    if st != QP_OK:
+        raise QuantPipeError(st, what)
 
 
 def _uint(v: int, what: str) -> int:
@@ -490,18 +495,19 @@ def qp_kv_attention_workspace_bytes(cache: qp_kv_cache_t, rows: qp_kv_rows_t, to
 
 
 def qp_kv_pool_init(n_pages: int, pool, stream=None) -> None:
-    _kv_call(pool.device, stream, "qp_kv_pool_init", int(n_pages), _ints(pool, 1, pool.device), pool.numel() * 4)
+    d = pool.get_device()
+    _kv_call(d, stream, "qp_kv_pool_init", int(n_pages), _ints(pool, 1, d), pool.numel() * 4)
+
+
+def _same_device(cache, rows) -> int:
+    if rows.device != cache.device:
+        raise ValueError("the rows are on device %d, the pages on device %d" % (rows.device, cache.device))
+    return cache.device
 
 
 def _books(what: str, cache, rows, pool, per_row, stream) -> None:
-    d = cache.tensors[0].device
-    _same_device(d, rows)
+    d = _same_device(cache, rows)
     _kv_call(d, stream, what, C.byref(cache), C.byref(rows), _ints(per_row, rows.rows, d), _ints(pool, 1, d), pool.numel() * 4)
-
-
-def _same_device(device, rows) -> None:
-    if rows.tensors[0].device != device:
-        raise ValueError("the rows are on %s, the pages on %s" % (rows.tensors[0].device, device))
 
 
 def qp_kv_reserve(cache, rows, pool, want, stream=None) -> None:
@@ -521,15 +527,13 @@ def qp_kv_free(cache, rows, pool, keep, stream=None) -> None:
 
 def qp_kv_compact(cache, rows, pool, stream=None) -> None:
     """Moves the pages in use to the pool's low end; word 3 of `pool` says how many there are."""
-    d = cache.tensors[0].device
-    _same_device(d, rows)
+    d = _same_device(cache, rows)
     _kv_call(d, stream, "qp_kv_compact", C.byref(cache), C.byref(rows), _ints(pool, 1, d), pool.numel() * 4)
 
 
 def qp_kv_append(cache, rows, layer: int, token_begin, k, v, stream=None) -> None:
     """Quantizes k, v [tokens, kv_heads, head_dim] into the rows' last places."""
-    d = cache.tensors[0].device
-    _same_device(d, rows)
+    d = _same_device(cache, rows)
     n = k.shape[0]
     kv, vv = _view(k, cache.kv_heads, cache.head_dim, n, d), _view(v, cache.kv_heads, cache.head_dim, n, d)
     _kv_call(d, stream, "qp_kv_append", C.byref(cache), C.byref(rows), _uint(layer, "qp_kv_append"), _ints(token_begin, rows.rows + 1, d), n, C.byref(kv), C.byref(vv))
@@ -537,8 +541,7 @@ def qp_kv_append(cache, rows, layer: int, token_begin, k, v, stream=None) -> Non
 
 def qp_kv_read(cache, rows, layer: int, token_begin, k, v, first=None, stream=None) -> None:
     """Writes the rows' tokens from first[r] (None: 0) on to k, v [tokens, kv_heads, head_dim]."""
-    d = cache.tensors[0].device
-    _same_device(d, rows)
+    d = _same_device(cache, rows)
     n = k.shape[0]
     kv, vv = _view(k, cache.kv_heads, cache.head_dim, n, d), _view(v, cache.kv_heads, cache.head_dim, n, d)
     f = None if first is None else _ints(first, rows.rows, d)
@@ -548,12 +551,11 @@ def qp_kv_read(cache, rows, layer: int, token_begin, k, v, first=None, stream=No
 def qp_kv_attention(cache, rows, layer: int, token_begin, q, out, ws, scale: float = None, causal: bool = True, window: int = 0,
                     stream=None) -> None:
     """out = softmax(scale q K^T) V for the rows' last tokens; q, out [tokens, q_heads, head_dim]; scale None: 1 / sqrt(head_dim)."""
-    d = cache.tensors[0].device
-    _same_device(d, rows)
+    d = _same_device(cache, rows)
     n, heads = q.shape[0], q.shape[1]
     qv, ov = _view(q, heads, cache.head_dim, n, d), _view(out, heads, cache.head_dim, n, d)
-    if ws.device != d or not ws.is_contiguous():
-        raise ValueError("expected a contiguous workspace on %s" % d)
+    if ws.get_device() != d or not ws.is_contiguous():
+        raise ValueError("expected a contiguous workspace on device %d" % d)
     cfg = qp_kv_attn_cfg_t(cache.head_dim ** -0.5 if scale is None else scale, heads, 1 if causal else 0, _uint(window, "qp_kv_attention"))
     _kv_call(d, stream, "qp_kv_attention", C.byref(cache), C.byref(rows), _uint(layer, "qp_kv_attention"), _ints(token_begin, rows.rows + 1, d), n, C.byref(qv), C.byref(ov),
              C.byref(cfg), ws.data_ptr(), ws.numel() * ws.element_size())
