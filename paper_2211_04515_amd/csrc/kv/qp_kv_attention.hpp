@@ -31,9 +31,9 @@
 //          LDS.  Prompts: bound by issue: 12 vector instructions for each score (3 for taking codes apart) beside two matrix ones for 16.
 // A call whose rows bring 16 columns or fewer on average goes to `few` alone; else rows are cut into 128 columns for `many`, and
 // a rest of 16 or fewer goes to `few` (single tokens in a batch with prompts).  Rows' lengths are known to the device only: every
-// block adds up the whole call's work from them (a few hundred lengths: one load a lane) and finds which item, and which of S
-// equal pieces of its tokens, is its own, so that about as many pieces come out as the chip runs at a time, whatever the
-// lengths.  Pieces leave (m, sum p, numerators) in the workspace, and a last kernel joins them in order.
+// wave adds up the whole call's work from them (a row a lane; of more than 64 rows a small kernel ahead does it once) and finds which
+// item, and which of S equal pieces of its tokens, is its block's, so that about as many pieces come out as the chip runs at a time,
+// whatever the lengths.  Pieces leave (m, sum p, numerators) in the workspace, and a last kernel joins them in order.
 //
 // Measured (bf16, heads of 128): one token each for 4 rows of up to 131072 (8 key heads, 64 of queries) 113 us, 4.9 TB/s, which is a large
 // copy's rate (4.7); for 32 rows of up to 4096 34 us, 3.0 TB/s, of which joining and finding work are 6; a prompt of 8192 tokens (4 key heads,
@@ -68,16 +68,19 @@ constexpr float kAtHeadroom = 8.0f;              // log2 that a score may lie ab
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-// A part of the workspace, for one kind of items: [0] columns that were split; a record for each; (m, sum) and numerators of the
-// pieces, in units of 16 columns.
+// A part of the workspace, for one kind of items: the header ([0] columns that were split, [1] tiles of a piece); with more rows than a
+// wave has lanes where the parts of each end; a record for each column that was split; (m, sum) and numerators of the pieces, in units of
+// 16 columns.
 struct AtWork {
     uint32_t *header;
+    u32x4 *ends;
     u32x4 *cols;
     float2 *sums;
     float *nums;
     uint32_t most_cols, most_units;
     uint32_t wide;                               // rows are cut into 128 columns first
     uint32_t slots;                              // blocks that run at the same time
+    uint32_t blocks;                             // of the launch
 };
 constexpr size_t kAtHeader = 256;
 // Columns that a wave of `few` shall not take one by one: see above.
@@ -101,11 +104,14 @@ template <bool MANY> AtWork at_work(char *ws, const KvLayer &c, uint32_t dim, ui
     w.slots = kAtSlots<MANY>;
     w.most_units = (uint32_t)(pieces * (kAtCols<MANY> / kAtUnit));
     w.most_cols = (uint32_t)cols;
-    const size_t sums = kAtHeader + (size_t)cols * sizeof(u32x4), nums = sums + (size_t)w.most_units * kAtUnit * sizeof(float2);
+    w.blocks = (uint32_t)(2u * slots + items);   // (pieces: see at_share; an item that is not cut up is one)
+    const size_t records = kAtHeader + (c.rows > (uint32_t)kWave ? (size_t)c.rows * sizeof(u32x4) : 0u);
+    const size_t sums = records + (size_t)cols * sizeof(u32x4), nums = sums + (size_t)w.most_units * kAtUnit * sizeof(float2);
     bytes = nums + (size_t)w.most_units * kAtUnit * dim * sizeof(float);
     if (ws) {
         w.header = reinterpret_cast<uint32_t *>(ws);
-        w.cols = reinterpret_cast<u32x4 *>(ws + kAtHeader);
+        w.ends = reinterpret_cast<u32x4 *>(ws + kAtHeader);
+        w.cols = reinterpret_cast<u32x4 *>(ws + records);
         w.sums = reinterpret_cast<float2 *>(ws + sums);
         w.nums = reinterpret_cast<float *>(ws + nums);
     }
@@ -146,31 +152,13 @@ struct AtPiece {
     uint32_t per;                                // tiles that a piece should have
     uint32_t unit, rec;                          // where the item's partial results and its columns' records go
 };
-// Inclusive prefix sums of three numbers over the block; `part` holds each wave's totals.
-__device__ __forceinline__ void at_scan(uint32_t (&x)[3], uint32_t (*part)[3], uint32_t (&total)[3])
+// Prefix sums that stay at kAtCap, which is more than any launch has, instead of passing 32 bits (rows that overlap can come to that).
+constexpr uint32_t kAtCap = 0x7fffffffu;
+__device__ __forceinline__ uint32_t at_plus(uint32_t x, uint32_t y) { return min(x + y, kAtCap); }
+__device__ __forceinline__ uint32_t at_wave_scan(uint32_t v)
 {
-    const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) x[i] = kv_wave_scan(x[i]);
-    if (lane == kWave - 1u)
-#pragma unroll
-        for (int i = 0; i < 3; ++i) part[wave][i] = x[i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-        total[i] = 0u;
-#pragma unroll
-        for (uint32_t w = 0; w < (uint32_t)kAtWaves; ++w) {
-            x[i] += w < wave ? part[w][i] : 0u;
-            total[i] += part[w][i];
-        }
-    }
-}
-__device__ __forceinline__ uint64_t at_wave_sum(uint64_t v)
-{
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) v += ((uint64_t)__shfl_xor((uint32_t)(v >> 32), d, kWave) << 32) + __shfl_xor((uint32_t)v, d, kWave);
-    return v;
+    const uint64_t sum = ((uint64_t)kv_wave_scan(v >> 16) << 16) + kv_wave_scan(v & 0xffffu);
+    return (uint32_t)min(sum, (uint64_t)kAtCap);
 }
 
 // What a row adds to the call: blocks, units of partial results, columns with records.
@@ -186,7 +174,7 @@ template <bool MANY> struct AtParts {
     // `e`: where its parts end among all rows'.  True where the rows' tokens do not overlap: what the host sized the grid and the workspace for.
     __device__ __forceinline__ bool fits(const AtWork &w, const uint32_t (&e)[3]) const
     {
-        return e[0] - blocks <= gridDim.x && e[0] <= gridDim.x && e[1] - units <= w.most_units && e[1] <= w.most_units && e[2] - cols <= w.most_cols &&
+        return e[0] - blocks <= w.blocks && e[0] <= w.blocks && e[1] - units <= w.most_units && e[1] <= w.most_units && e[2] - cols <= w.most_cols &&
                e[2] <= w.most_cols;
     }
     // the row's block i
@@ -236,7 +224,7 @@ template <bool MANY> __device__ __forceinline__ bool at_find(const KvLayer &c, c
         const uint64_t items = (uint64_t)wave_sum_u32(o.items) * c.kv_heads;
         const uint32_t per = at_share(cost, items, w.slots, [&](uint32_t p) { return (uint64_t)wave_sum_u32(o.items * ((o.tiles + p - 1u) / p)) * c.kv_heads; });
         const AtParts<MANY> parts(c, o, per);
-        const uint32_t e[3] = {kv_wave_scan(parts.blocks), kv_wave_scan(parts.units), kv_wave_scan(parts.cols)};
+        const uint32_t e[3] = {at_wave_scan(parts.blocks), at_wave_scan(parts.units), at_wave_scan(parts.cols)};
         const bool fits = parts.fits(w, e);
         if (block == 0u && tid < (uint32_t)kWave) {
             const uint32_t split = wave_max_u32(fits && parts.cols != 0u ? e[2] : 0u);
@@ -253,45 +241,90 @@ template <bool MANY> __device__ __forceinline__ bool at_find(const KvLayer &c, c
         mine = its.piece(c, row, (uint32_t)from, per, end, block - (end[0] - its.blocks));
         return true;
     }
-    __shared__ uint32_t part[kAtWaves][3];
-    __shared__ uint64_t work[kAtWaves];
-    __shared__ AtPiece found;
-    __shared__ uint32_t have, split;
-    const AtRow mine0 = at_row<MANY>(c, a, w.wide, min(tid, c.rows - 1u));          // (most calls have no more rows than that)
-    uint64_t cost = tid < c.rows ? (uint64_t)mine0.tiles * mine0.items : 0u;
-    for (uint32_t r = tid + kAtThreads; r < c.rows; r += kAtThreads) {
+    // k_kv_plan has been here: the first row that ends behind the block, 64 of them at a time
+    uint32_t r = 0, n = c.rows;
+    while (true) {
+        const uint32_t step = (n + kWave - 1u) / kWave, at = lane * step;
+        const uint32_t under = (uint32_t)__popcll(__ballot(at < n && w.ends[r + min(at, n - 1u)][0] <= block));
+        if (under == 0u) break;
+        r += (under - 1u) * step;
+        n = min(step, c.rows - r);
+        if (step == 1u) {
+            ++r;
+            break;
+        }
+    }
+    if (r >= c.rows) return false;
+    const u32x4 ends = w.ends[r];
+    const uint32_t end[3] = {ends[0], ends[1], ends[2]}, per = w.header[1];
+    const AtRow row = at_row<MANY>(c, a, w.wide, r);
+    const AtParts<MANY> its(c, row, per);
+    if (!its.fits(w, end) || block < end[0] - its.blocks || block >= end[0]) return false;
+    mine = its.piece(c, row, r, per, end, block - (end[0] - its.blocks));
+    return true;
+}
+
+__device__ __forceinline__ uint64_t at_wave_sum(uint64_t v)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) v += ((uint64_t)__shfl_xor((uint32_t)(v >> 32), d, kWave) << 32) + __shfl_xor((uint32_t)v, d, kWave);
+    return v;
+}
+
+// With more rows than a wave has lanes, one block for each kind of items adds the rows up ahead of them: else every block would, and 4096 rows
+// of up to 500 tokens took 1356 us, so 580; 20000 of 200 17.6 ms, so 2.0; 1024 of 1000 302, so 251; 96 of 1000 30, so 34, which is the launch.
+constexpr uint32_t kAtPlan = 1024;
+template <bool MANY> __device__ __forceinline__ void at_plan(const KvLayer &c, const KvAttn &a, const AtWork &w)
+{
+    __shared__ uint64_t work[kAtPlan / kWave];
+    __shared__ uint32_t part[kAtPlan / kWave][3];
+    __shared__ uint32_t split;
+    const uint32_t tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    uint64_t cost = 0;
+    for (uint32_t r = tid; r < c.rows; r += kAtPlan) {
         const AtRow o = at_row<MANY>(c, a, w.wide, r);
         cost += (uint64_t)o.tiles * o.items;
     }
     cost = at_wave_sum(cost);
-    if (lane == 0u) work[tid / kWave] = cost;
-    if (tid == 0u) have = split = 0u;
+    if (lane == 0u) work[wave] = cost;
+    if (tid == 0u) split = 0u;
     __syncthreads();
+    cost = 0;
+    for (uint32_t i = 0; i < kAtPlan / kWave; ++i) cost += work[i];
     // (many rows: their mean piece is taken for what is lost at their ends)
-    const uint32_t per = at_share((work[0] + work[1] + work[2] + work[3]) * c.kv_heads * 5u / 4u, 4u * (uint64_t)w.slots, w.slots, [](uint32_t) { return 0ull; });
-    uint32_t before[3] = {0u, 0u, 0u};                   // blocks, units, columns of the rows so far
-    for (uint32_t r0 = 0; r0 < c.rows; r0 += kAtThreads) {
+    const uint32_t per = at_share(cost * c.kv_heads * 5u / 4u, 4u * (uint64_t)w.slots, w.slots, [](uint32_t) { return 0ull; });
+    uint32_t before[3] = {0u, 0u, 0u};           // blocks, units, columns of the rows so far
+    for (uint32_t r0 = 0; r0 < c.rows; r0 += kAtPlan) {
         const uint32_t r = r0 + tid;
-        const AtRow o = r >= c.rows ? none : r0 == 0u ? mine0 : at_row<MANY>(c, a, w.wide, r);
+        AtRow o{};
+        o.tiles = 1u;
+        if (r < c.rows) o = at_row<MANY>(c, a, w.wide, r);
         const AtParts<MANY> parts(c, o, per);
-        uint32_t e[3] = {parts.blocks, parts.units, parts.cols}, total[3];
-        at_scan(e, part, total);
-#pragma unroll
-        for (int k = 0; k < 3; ++k) e[k] += before[k];
-        const bool fits = parts.fits(w, e);
-        if (fits && parts.cols != 0u) atomicMax(&split, e[2]);
-        if (fits && block >= e[0] - parts.blocks && block < e[0]) {
-            found = parts.piece(c, o, r, per, e, block - (e[0] - parts.blocks));
-            have = 1u;
-        }
-#pragma unroll
-        for (int k = 0; k < 3; ++k) before[k] += total[k];
+        uint32_t e[3] = {at_wave_scan(parts.blocks), at_wave_scan(parts.units), at_wave_scan(parts.cols)};
+        if (lane == kWave - 1u)
+            for (int k = 0; k < 3; ++k) part[wave][k] = e[k];
         __syncthreads();
-        if (block < before[0] && block != 0u) break;     // (block 0 goes on: it says how many columns were split)
+        for (int k = 0; k < 3; ++k) {
+            uint32_t all = before[k];
+            for (uint32_t i = 0; i < kAtPlan / kWave; ++i) {
+                if (i == wave) e[k] = at_plus(e[k], all);
+                all = at_plus(all, part[i][k]);
+            }
+            before[k] = all;
+        }
+        if (r < c.rows) w.ends[r] = u32x4{e[0], e[1], e[2], 0u};
+        if (parts.cols != 0u && parts.fits(w, e)) atomicMax(&split, e[2]);
+        __syncthreads();                         // (the sums are used again)
     }
-    if (block == 0u && tid == 0u) w.header[0] = split;
-    mine = found;
-    return have != 0u;
+    if (tid == 0u) {
+        w.header[0] = split;
+        w.header[1] = per;
+    }
+}
+template <int D> __global__ __launch_bounds__(kAtPlan) void k_kv_plan(KvLayer c, KvAttn a, AtWork few, AtWork many)
+{
+    if (blockIdx.x == 0u) at_plan<false>(c, a, few);
+    else at_plan<true>(c, a, many);
 }
 
 // The pages of a row, 64 at a time: lane i has slot base + i's.  (A load for each would be waited for in each step: 600 cycles.)
@@ -1088,13 +1121,16 @@ static hipError_t at_launch(const KvLayer &c, const KvView &q, const KvView &out
         few.slots = kAtSlots<false> * 2u / 3u;
         many.slots = kAtSlots<true> / 2u;
     }
-    // (pieces: see at_share; an item that is not cut up is one)
     hipError_t e;
-    if (wide) {
-        hipLaunchKernelGGL((k_kv_attention_many<D, DT>), dim3((unsigned)(2u * kAtSlots<true> + at_items<true>(c, a.group))), dim3(kAtThreads), 0, s, c, q, out, a, many);
+    if (c.rows > (uint32_t)kWave) {
+        hipLaunchKernelGGL(k_kv_plan<D>, dim3(wide ? 2u : 1u), dim3(kAtPlan), 0, s, c, a, few, many);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((k_kv_attention_few<D, DT>), dim3((unsigned)(2u * kAtSlots<false> + at_items<false>(c, a.group))), dim3(kAtThreads), 0, s, c, q, out, a, few);
+    if (wide) {
+        hipLaunchKernelGGL((k_kv_attention_many<D, DT>), dim3(many.blocks), dim3(kAtThreads), 0, s, c, q, out, a, many);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((k_kv_attention_few<D, DT>), dim3(few.blocks), dim3(kAtThreads), 0, s, c, q, out, a, few);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const uint32_t cols = few.most_cols + many.most_cols;
     if (cols == 0u) return hipSuccess;        // no row is longer than a piece

@@ -150,6 +150,17 @@ def test_many_rows(qp):
     Case(qp, 64, 32, 1, lengths.tolist()).attend(counts.tolist(), 2, "bf16")
 
 
+def test_thousands_of_rows(qp):
+    """One token each of 3000 rows, and prompts among them: where each row's work begins is found ahead of it."""
+    rng = np.random.default_rng(9)
+    lengths = rng.integers(0, 12, 3000)
+    lengths[[5, 1023, 1024, 2999]] = 700, 300, 90, 64
+    counts = np.minimum(lengths, 1)
+    Case(qp, 64, 32, 1, lengths.tolist(), per_row=22).attend(counts.tolist(), 1, "bf16")
+    counts[[5, 1024, 2999]] = 150, 90, 33
+    Case(qp, 64, 32, 2, lengths.tolist(), per_row=22).attend(counts.tolist(), 32, "f32")
+
+
 def test_scores_that_spread_far(qp):
     """Softmax from next to one-hot to flat, maxima that come late, queries that are tiny, huge, zero, or not finite."""
     c = Case(qp, 64, 32, 2, [1300, 1300])
