@@ -487,7 +487,7 @@ def qp_kv_page_bytes(cache: qp_kv_cache_t) -> int:
 
 
 def qp_kv_pool_bytes(n_pages: int) -> int:
-    return int(lib().qp_kv_pool_bytes(int(n_pages)))
+    return int(lib().qp_kv_pool_bytes(int(n_pages))) if 0 <= n_pages < 1 << 32 else 0
 
 
 def qp_kv_attention_workspace_bytes(cache: qp_kv_cache_t, rows: qp_kv_rows_t, tokens: int, q_heads: int) -> int:

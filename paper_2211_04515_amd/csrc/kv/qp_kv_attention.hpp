@@ -30,14 +30,14 @@
 //   many   128 columns, 32 a wave; all waves the same tokens, whose words each wave takes apart a quarter of and shares through
 //          LDS.  Prompts: bound by issue: 12 vector instructions for each score (3 for taking codes apart) beside two matrix ones for 16.
 // A call whose rows bring 16 columns or fewer on average goes to `few` alone; else rows are cut into 128 columns for `many`, and
-// a rest of 16 or fewer goes to `few` (single tokens in a batch with prompts).  Rows' lengths are known to the device only: every
+// a rest of 16 or fewer goes to `few`, in the same launch (single tokens in a batch with prompts).  Rows' lengths are known to the device only: every
 // wave adds up the whole call's work from them (a row a lane; of more than 64 rows a small kernel ahead does it once) and finds which
 // item, and which of S equal pieces of its tokens, is its block's, so that about as many pieces come out as the chip runs at a time,
 // whatever the lengths.  Pieces leave (m, sum p, numerators) in the workspace, and a last kernel joins them in order.
 //
 // Measured (bf16, heads of 128): one token each for 4 rows of up to 131072 (8 key heads, 64 of queries) 113 us, 4.9 TB/s, which is a large
 // copy's rate (4.7); for 32 rows of up to 4096 34 us, 3.0 TB/s, of which joining and finding work are 6; a prompt of 8192 tokens (4 key heads,
-// 16 of queries) 366 us, 750 TFLOP/s, where a large library product in fp16 runs at 1220: vector instructions take 61 % of the SIMDs'
+// 16 of queries) 362 us, 760 TFLOP/s, where a large library product in fp16 runs at 1220: vector instructions take 61 % of the SIMDs'
 // cycles and matrix ones 36 %.
 #pragma once
 
@@ -720,9 +720,9 @@ __device__ __forceinline__ void at_range(const KvRow &row, const KvAttn &a, uint
     hi = a.causal ? (uint32_t)max((int64_t)0, min(last + 1, (int64_t)row.length)) : (uint32_t)row.length;
     if (lo > hi) lo = hi;
 }
-template <bool MANY> __device__ __forceinline__ bool at_begin(const KvLayer &c, const KvAttn &a, const AtWork &w, AtBlock &b)
+template <bool MANY> __device__ __forceinline__ bool at_begin(const KvLayer &c, const KvAttn &a, const AtWork &w, uint32_t block, AtBlock &b)
 {
-    if (!at_find<MANY>(c, a, w, blockIdx.x, b.p)) return false;
+    if (!at_find<MANY>(c, a, w, block, b.p)) return false;
     AtPiece &p = b.p;
     p.row = __builtin_amdgcn_readfirstlane(p.row);
     p.head = __builtin_amdgcn_readfirstlane(p.head);
@@ -806,17 +806,22 @@ __device__ __forceinline__ void at_store(const AtWave<D, NCT, DT> &x, const AtBl
     }
 }
 
+// LDS of a block with few columns: two waves' numerators and (m, sum) when the four are joined; the grids of each wave's step.
+template <int D> struct AtFewLds {
+    float nums[2][16][D + 4];
+    float2 grids[kAtWaves][64];
+    float2 sums[2][16];
+};
 template <int D, int DT>
-__global__ __launch_bounds__(kAtThreads, D <= 128 ? 2 : 1) void k_kv_attention_few(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
+__device__ __forceinline__ void at_few(const KvLayer &c, const KvView &qv, const KvView &out, const KvAttn &a, const AtWork &w, uint32_t block, AtFewLds<D> &lds)
 {
     using Wave = AtWave<D, 1, DT>;
     constexpr int NB = Wave::NB;
-    // two waves' numerators and (m, sum) when the four are joined; the grids of each wave's step
-    __shared__ __align__(16) float nums[2][16][D + 4];
-    __shared__ float2 sums[2][16];
-    __shared__ __align__(16) float2 grids[kAtWaves][64];
+    float (&nums)[2][16][D + 4] = lds.nums;
+    float2 (&sums)[2][16] = lds.sums;
+    float2 (&grids)[kAtWaves][64] = lds.grids;
     AtBlock b;
-    if (!at_begin<false>(c, a, w, b)) return;
+    if (!at_begin<false>(c, a, w, block, b)) return;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u;
     AtPages pages;
     const auto slab_at = [&](uint32_t t, bool &there) {
@@ -890,20 +895,29 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 ? 2 : 1) void k_kv_attention_f
 }
 
 template <int D, int DT>
-__global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? 2 : 1) void k_kv_attention_many(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
+__global__ __launch_bounds__(kAtThreads, D <= 128 ? 2 : 1) void k_kv_attention_few(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
+{
+    __shared__ __align__(16) AtFewLds<D> lds;
+    at_few<D, DT>(c, qv, out, a, w, blockIdx.x, lds);
+}
+
+// Of 32 tokens: the fragments of keys (j, k), then of values, and the grids.
+template <int D> struct AtStage {
+    f16x8 frags[2 * ((D + 31) / 32) + D / 16][kWave];
+    float2 grids[64];
+};
+template <int D> constexpr uint32_t kAtSub = D <= 128 ? 2 : 1;      // of them between two barriers
+template <int D, int DT>
+__device__ __forceinline__ void at_many(const KvLayer &c, const KvView &qv, const KvView &out, const KvAttn &a, const AtWork &w, uint32_t block,
+                                        AtStage<D> (&stages)[2][kAtSub<D>])
 {
     constexpr int NCT = 2;
     using Wave = AtWave<D, NCT, DT>;
+    using Stage = AtStage<D>;
     constexpr int NB = Wave::NB, KS = Wave::KS;
-    constexpr uint32_t kFrags = 2 * KS + NB;                        // fragments of 32 tokens: keys (j, k), then values
-    constexpr uint32_t kSub = D <= 128 ? 2 : 1, kStage = kSub * kAtStep;      // tokens between two barriers
-    struct Stage {
-        f16x8 frags[kFrags][kWave];
-        float2 grids[64];
-    };
-    __shared__ __align__(16) Stage stages[2][kSub];
+    constexpr uint32_t kSub = kAtSub<D>, kStage = kSub * kAtStep;
     AtBlock b;
-    if (!at_begin<true>(c, a, w, b)) return;
+    if (!at_begin<true>(c, a, w, block, b)) return;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, g = lane / 16u, n = lane % 16u;
     const uint32_t col0 = min(b.p.col0 + wave * 16u * NCT, b.p.col1), col1 = min(col0 + 16u * NCT, b.p.col1);
     const AtMagic magic;
@@ -997,6 +1011,20 @@ __global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? 2 : 1) void
     }
     x.finish();
     at_store<D, NCT, DT>(x, b, a, w, out, kAtCols<true>, col0, col1);
+}
+
+// Both kinds at once: the rests that are for `few` come behind the others, beside their last work (a launch of their own: 4 rows
+// of 130 new tokens and 1000 in all 58 us, so 47; a prompt of 2048 among 63 single tokens 155, so 148).
+template <int D, int DT>
+__global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? 2 : 1) void k_kv_attention_many(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork few, AtWork many)
+{
+    union Lds {
+        AtFewLds<D> few;
+        AtStage<D> many[2][kAtSub<D>];
+    };
+    __shared__ __align__(16) unsigned char lds[sizeof(Lds)];
+    if (blockIdx.x < many.blocks) at_many<D, DT>(c, qv, out, a, many, blockIdx.x, *reinterpret_cast<AtStage<D>(*)[2][kAtSub<D>]>(lds));
+    else at_few<D, DT>(c, qv, out, a, few, blockIdx.x - many.blocks, *reinterpret_cast<AtFewLds<D> *>(lds));
 }
 
 // ---- the pieces of a column, joined ----------------------------------------------------------------------------------------
@@ -1126,11 +1154,8 @@ static hipError_t at_launch(const KvLayer &c, const KvView &q, const KvView &out
         hipLaunchKernelGGL(k_kv_plan<D>, dim3(wide ? 2u : 1u), dim3(kAtPlan), 0, s, c, a, few, many);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    if (wide) {
-        hipLaunchKernelGGL((k_kv_attention_many<D, DT>), dim3(many.blocks), dim3(kAtThreads), 0, s, c, q, out, a, many);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL((k_kv_attention_few<D, DT>), dim3(few.blocks), dim3(kAtThreads), 0, s, c, q, out, a, few);
+    if (wide) hipLaunchKernelGGL((k_kv_attention_many<D, DT>), dim3(many.blocks + few.blocks), dim3(kAtThreads), 0, s, c, q, out, a, few, many);
+    else hipLaunchKernelGGL((k_kv_attention_few<D, DT>), dim3(few.blocks), dim3(kAtThreads), 0, s, c, q, out, a, few);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const uint32_t cols = few.most_cols + many.most_cols;
     if (cols == 0u) return hipSuccess;        // no row is longer than a piece

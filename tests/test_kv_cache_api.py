@@ -180,3 +180,5 @@ def test_the_binding_refuses_tensors_of_other_kinds(qp):
         qp.alloc_kv_pages(4, 1, 65, 32, device="cpu")
     with pytest.raises(qp.QuantPipeError):
         qp.alloc_kv_pool(0, device="cpu")
+    with pytest.raises(qp.QuantPipeError):
+        qp.alloc_kv_pool(2 ** 32 + 5, device="cpu")
