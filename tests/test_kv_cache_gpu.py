@@ -496,6 +496,45 @@ def test_a_serving_loop(qp, dtype):
     step([33, 0, 1, 1, 1, 2])
 
 
+def test_as_many_rows_as_there_may_be(qp):
+    """65536 rows, two tokens each, in two steps.  fp32: the weights of two tokens are off by at most (dim + 8) roundings of 2^-24 of a score
+    below 64 in size, so 2^-11 of one (72 * 64 * 2^-24 < 2^-11), and the answer by that times the values' spread.  Its two parts, of
+    (c - 8) s and of lo + 8 s, cancel where an element is small: they are rounded as they are, and with T the largest of the tokens' values
+    15 s <= 2 T and -T <= lo <= T, so both are at most 1.1 T; weights in two halves (2^-22) and three sums of two (2^-24 each) for both
+    parts come to less than 2 * 1.1 * (2^-22 + 3 * 2^-24) T < 2^-20 T."""
+    rows, dim, page = 65536, 64, 32
+    pages = qp.alloc_kv_pages(rows + 9, 1, dim, page)
+    cache, pool = qp.kv_cache(pages, 1, dim, page), qp.alloc_kv_pool(rows + 9)
+    table, lengths = torch.full((rows, 1), -1, dtype=torch.int32, device="cuda"), torch.zeros(rows, dtype=torch.int32, device="cuda")
+    r = qp.kv_rows(table, lengths)
+    begin = torch.arange(rows + 1, dtype=torch.int32, device="cuda")
+    g = torch.Generator("cuda").manual_seed(8)
+    ws = qp.alloc_kv_workspace(cache, r, rows, 2)
+    for step in (1, 2):
+        qp.qp_kv_reserve(cache, r, pool, torch.ones(rows, dtype=torch.int32, device="cuda"))
+        assert pool[:2].tolist() == [0, 0] and (lengths == step).all()
+        k, v, q = (torch.randn(rows, n, dim, device="cuda", generator=g) for n in (1, 1, 2))
+        out = torch.empty_like(q)
+        qp.qp_kv_append(cache, r, 0, begin, k, v)
+        qp.qp_kv_attention(cache, r, 0, begin, q, out, ws)
+    assert torch.equal(table.view(-1), begin[:-1])                # (in order: the lowest free page first)
+    ko, vo = (torch.empty(2 * rows, 1, dim, device="cuda") for _ in range(2))
+    qp.qp_kv_read(cache, r, 0, 2 * begin, ko, vo)
+    ko, vo, q = ko.view(rows, 1, 2, dim).double(), vo.view(rows, 1, 2, dim).double(), q.double()
+    scores = (q.unsqueeze(2) * ko).sum(-1) * dim ** -0.5
+    assert scores.abs().max() < 64
+    want = (torch.softmax(scores, -1).unsqueeze(-1) * vo).sum(2)
+    off, spread, top = (out.double() - want).abs(), (vo[:, :, 0] - vo[:, :, 1]).abs(), vo.abs().amax((2, 3)).unsqueeze(-1)
+    worst = (off / (spread * 2.0 ** -11 + top * 2.0 ** -20)).max()
+    assert worst <= 1, worst
+    qp.qp_kv_free(cache, r, pool, torch.where(begin[:-1] % 2 == 0, 0, -1).int())
+    qp.qp_kv_compact(cache, r, pool)
+    assert int(pool[3]) == rows // 2 and int(table[1::2].max()) < rows // 2 and (table[::2] == -1).all()
+    k2, v2 = (torch.empty(rows, 1, dim, device="cuda") for _ in range(2))
+    qp.qp_kv_read(cache, r, 0, torch.cat([torch.zeros(1, device="cuda"), (2 * (begin[:-1] % 2)).cumsum(0)]).int(), k2, v2)
+    assert torch.equal(k2.view(rows // 2, 2, dim).double(), ko[1::2, 0]) and torch.equal(v2.view(rows // 2, 2, dim).double(), vo[1::2, 0])
+
+
 def test_a_step_replays_from_a_graph(qp):
     """Reserve, append, attention and free of one step in a captured graph, replayed with other inputs between the program's own eager
     calls, each replay against the same calls made eagerly on a copy."""

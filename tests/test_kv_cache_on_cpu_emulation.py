@@ -192,6 +192,22 @@ def test_token_ranges_that_make_no_sense_stay_inside(driver, tmp_path, begin):
     e.run("o")
 
 
+def test_ranges_of_many_rows_that_overlap_stay_inside(driver, tmp_path):
+    """More rows than a wave has lanes, of which every second one has all of the call's tokens: far more work than the launch is for."""
+    rng = np.random.default_rng(2)
+    heads, dim, page, rows, per_row, n_pages, tokens = 1, 64, 32, 70, 6, 5, 30
+    e = Emu(driver, tmp_path)
+    q = rng.standard_normal((tokens, 2 * heads, dim)).astype(np.float32)
+    begin = np.where(np.arange(rows + 1) % 2, tokens, 0).astype(np.int32)
+    for n, a in (("pages", kp.new_pages(1, n_pages, heads, dim, page)), ("table", rng.integers(-2, n_pages + 2, (rows, per_row)).astype(np.int32)),
+                 ("lengths", rng.integers(-9, 400, rows).astype(np.int32)), ("begin", begin), ("q", q), ("o", q)):
+        e.buf(n, a)
+    e.do("cache", "pages", 1, n_pages, heads, dim, page)
+    e.do("rows", "table", "lengths", rows, per_row)
+    e.do("attention", 0, "begin", tokens, "q", "o", 0, 2 * heads * dim, dim, 2 * heads, 0.125, 1, 0)
+    e.run("o")
+
+
 # ---- attention -----------------------------------------------------------------------------------------------------------
 
 def attend(driver, path, dim, page, heads, group, lengths, counts, dtype, causal=1, window=0, scale=None, spoil=None, per_row=None, missing=()):
