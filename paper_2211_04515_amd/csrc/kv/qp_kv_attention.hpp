@@ -2,16 +2,19 @@
 //
 // Mathematics.  With key t = lo + c s (per token and head: codes c, grid lo, s) a score is a dot product with codes,
 //     scale q.k_t = scale (s_t sum_d q_d (c_td - 8) + (lo_t + 8 s_t) sum_d q_d),
-// and with p_t = exp(score_t - m) the answer's numerator is
+// and with p_t = 2^(score_t - m), scores in log2, the answer's numerator is
 //     sum_t p_t v_t = sum_t (p_t s_t) (c_t - 8) + sum_t p_t (lo_t + 8 s_t),
 // the second term the same for all elements of a head.  So both products run on the codes themselves: c - 8 is an integer in
 // [-8, 7], exact in fp16, and no value is ever dequantized.  (Centred codes, because the rounding of p_t s_t is multiplied by
 // them: -8..7 costs about as much as the values' own spread would.)
 //   q          is taken as 16 q in fp16: exact for bf16 (what is below 2^-14 rounds at 2^-29); fp32 is split in two halves, 22 bits
 //              of each element.  A column whose largest element lies outside [2^-4, 2^11) gets a power of two of its own.
-//   p_t s_t    is rounded to fp16 (fp32: split in two).  s_t is normalised by a power of two N so that the largest one seen lies
-//              in [2^5, 2^7], and p_t <= 2^8, so that nothing overflows and what is lost at the lower end is 2^-32 of the largest.
-//   Scores, the running maximum m, sum p_t, sum p_t (lo_t + 8 s_t) and the accumulators are fp32.
+//   p_t s_t    is rounded to fp16 (fp32: split in two).  m is no maximum of the scores but the column's own reference, such that the largest p_t s_t
+//              that it has seen lies between 2^6, when m was last moved, and 2^15.6: nothing overflows, and what is lost at the lower end is 2^-31 of
+//              the largest.  Of the tokens that the column sees, with the weight that it gives them: one reference for all columns of a wave, or one
+//              from the scales alone, lets a token with a vast value take the bits of columns that do not see or weigh it.  p_t itself stays
+//              below 2^96, which sums in fp32 hold; value scales below 2^-82 have fewer bits for it.
+//   Scores, sum p_t, sum p_t (lo_t + 8 s_t) and the accumulators are fp32.  m is a whole number, so that moving it rounds nothing.
 //
 // Matrix shape.  v_mfma_f32_16x16x32_f16 with S^T = K q^T (16 tokens x 16 columns; a column is one token of the call and one of the
 // query heads that share the key head) and O^T = V^T p^T.  With 32 tokens at a time, tile row m of the first product's two
@@ -20,9 +23,10 @@
 // element for the same reason; elements are dealt out as d = m NB + block so that a lane's words are next to each other.
 // A word w becomes eight halves as ((w >> 8 i) & 0x000f000f | 0x6400 6400) - 1032 and (.. & 0x00f000f0 | 0x5400 5400) - 72: codes
 // 0, 4, 1, 5, 2, 6, 3, 7; queries and p are put in the same order.
-// The maximum is lazy: a column's m moves only when a lane sees a score more than 8 (in log2) above it, so the loop has no exchange
-// between lanes; what is rare (the maximum moves, N moves) is one branch of the whole wave.  Scores are made relative to m in the step
-// that applies the grid, with scale log2(e) / 16 in the grid already: two instructions for a score, and the exponential's argument is there.
+// The reference is lazy: m moves only when p s would pass fp16, so the loop has no exchange between lanes; what is rare is one branch of the whole
+// wave, entered if a lane's largest score and its tokens' largest scale could do that together, and there each column decides for itself.  Scores are
+// made relative to m in the step that applies the grid, with scale log2(e) / 16 in the grid already: two instructions for a score, and the
+// exponential's argument is there.
 //
 // Who does what.  An item is some columns of one row and key head, a block (four waves) takes an item or a piece of its tokens:
 //   few    16 columns; every wave all of them and every fourth 32 tokens, joined through LDS at the end.  What a single token of a
@@ -33,7 +37,7 @@
 // a rest of 16 or fewer goes to `few`, in the same launch (single tokens in a batch with prompts).  Rows' lengths are known to the device only: every
 // wave adds up the whole call's work from them (a row a lane; of more than 64 rows a small kernel ahead does it once) and finds which
 // item, and which of S equal pieces of its tokens, is its block's, so that about as many pieces come out as the chip runs at a time,
-// whatever the lengths.  Pieces leave (m, sum p, numerators) in the workspace, and a last kernel joins them in order.
+// whatever the lengths.  Pieces leave (m, sum p, numerators) in the workspace, sum p brought to [1/2, 1), and a last kernel joins them in order.
 //
 // Measured (bf16, heads of 128): one token each for 4 rows of up to 131072 (8 key heads, 64 of queries) 113 us, 4.9 TB/s, which is a large
 // copy's rate (4.7); for 32 rows of up to 4096 34 us, 3.0 TB/s, of which joining and finding work are 6; a prompt of 8192 tokens (4 key heads,
@@ -63,7 +67,9 @@ template <bool MANY> constexpr uint32_t kAtSlots = MANY ? QP_KV_MANY : QP_KV_FEW
 #define QP_KV_LEAST 4
 #endif
 constexpr uint32_t kAtLeast = QP_KV_LEAST;
-constexpr float kAtHeadroom = 8.0f;              // log2 that a score may lie above its column's m
+// A column's reference, in log2: p = 2^(score - m) may be up to 2^kAtMost, so that sums stay in fp32, and p times the token's value scale up to
+// 2^kAtFull, so that it fits fp16; where one would pass, m rises to where the one is 2^kAtFar at most and the other 2^kAtRoom.
+constexpr float kAtMost = 96.0f, kAtFar = 89.0f, kAtFull = 15.5f, kAtRoom = 8.0f;
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -376,6 +382,10 @@ __device__ __forceinline__ f16x8 at_codes(uint32_t w, const AtMagic &k)
     return f16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
 }
 __device__ __forceinline__ float at_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+// 2^x for whole numbers x up to 127; 0 below -126.
+__device__ __forceinline__ float at_power(float x) { return x < -126.0f ? 0.0f : __uint_as_float((uint32_t)((int32_t)x + 127) << 23); }
+// log2 of x >= 0, between whole numbers on a straight line, which is 0.09 too low at most and never falls as x grows (0: -127); and its sum with y.
+__device__ __forceinline__ float at_log2_plus(float x, float y) { return fmaf((float)__float_as_uint(x), 0x1p-23f, y - 127.0f); }
 
 template <int D, int NCT, int DT> struct AtWave {
     static constexpr int KS = (D + 31) / 32;         // words of a lane of a key, and steps of the first product
@@ -383,13 +393,11 @@ template <int D, int NCT, int DT> struct AtWave {
     static constexpr int PIECES = DT == QP_F32 ? 2 : 1;
     f16x8 q[NCT][PIECES][KS];
     f32x4 o[NCT][NB];
-    float m[NCT], bq[NCT], l[NCT], lv[NCT];          // m in log2
-    float over[NCT];                                 // above it a score moves m: the headroom, or -inf while nothing was seen
+    float m[NCT], bq[NCT], l[NCT], lv[NCT];          // m: the column's reference, a whole number
+    float over[NCT];                                 // what a score relative to m may be: kAtMost, or -inf while nothing was seen
     float own[NCT];                                  // the column's own power of two
     bool owns;                                       // any column of the wave has one
     int32_t lo[NCT], hi[NCT];                        // the tokens that this lane's column sees
-    float norm, sv_most;                             // N, and the largest value scale that it is good for
-    int32_t norm_exp;
 
     struct Raw {
         uint32_t k[2][KS], v[NB];
@@ -475,9 +483,6 @@ template <int D, int NCT, int DT> struct AtWave {
         const int64_t pos = (int64_t)row.length - row.count + i;
         hi[t] = !is ? 0x7fffffff : a.causal ? (int32_t)max((int64_t)0, min(pos + 1, (int64_t)row.length)) : row.length;
         lo[t] = is && a.window ? (int32_t)max((int64_t)0, pos - (int64_t)a.window + 1) : 0;
-        norm = 1.0f;
-        norm_exp = 0;
-        sv_most = 0.0f;
     }
 
     // Where a lane's words and grid of 32 tokens lie, in bytes from the head's slab + (first token's slot) * D / 2 (the grid: + 8 of the
@@ -503,36 +508,44 @@ template <int D, int NCT, int DT> struct AtWave {
         x.written = there && (int32_t)(t0 + threadIdx.x % 32u) < length;
     }
 
-    // The maximum or N moves.
-    // `s`: scores relative to m, which follow
-    template <int SUB> __device__ __forceinline__ void rescale(f32x4 (&s)[SUB][NCT][2], const float (&top)[NCT], float sv_top)
+    // The references of the columns that have to be raised.  Each column's own scores and the scales of the tokens that it sees decide (the others'
+    // scores are -inf here), so that an answer is the same to the bit whatever the wave's other columns do.
+    // `s`: scores relative to m, which follow; `top`: this lane's largest ones; `mem`: as in weigh
+    template <int SUB, typename Mem> __device__ __forceinline__ void raise(f32x4 (&s)[SUB][NCT][2], const float (&top)[NCT], const Mem &mem)
     {
-        sv_top = fmaxf(sv_top, kv_xor_f32(sv_top, 16));
-        sv_top = fmaxf(sv_top, kv_xor_f32(sv_top, 32));
-        float ratio = 1.0f;
-        if (sv_top > sv_most) {          // (the same in all lanes)
-            int32_t ex;
-            (void)frexpf(sv_top, &ex);
-            const int32_t now = 6 - ex;
-            ratio = sv_most > 0.0f ? ldexpf(1.0f, now - norm_exp) : 1.0f;
-            norm_exp = now;
-            norm = ldexpf(1.0f, now);
-            sv_most = ldexpf(1.0f, ex + 1);
-        }
+        const uint32_t g = threadIdx.x % kWave / 16u;
 #pragma unroll
         for (int t = 0; t < NCT; ++t) {
-            float x = fmaxf(top[t], kv_xor_f32(top[t], 16));
-            x = fmaxf(x, kv_xor_f32(x, 32));
-            const bool first = over[t] < 0.0f;
-            const float next = x == -INFINITY ? m[t] : m[t] + (first ? x : fmaxf(x, 0.0f)), up = next - m[t];   // (what m moves by once rounded)
-            over[t] = x == -INFINITY ? over[t] : kAtHeadroom;
-            const float alpha = first ? 1.0f : at_exp2(-up);                          // (first: there is nothing to scale)
-            m[t] = next;
-            l[t] *= alpha;
-            lv[t] *= alpha;
-            const float beta = alpha * ratio;
+            // log2 of the largest p s, and of the largest p times what counts as a token's size: |lo + 8 s| too, far down, for lv's sake
+            float x = top[t], weight = -INFINITY, size = -INFINITY;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) o[t][b] *= beta;
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float2 gv = mem(u)[32u + 8u * g + i];
+                    const float at = s[u][t][i / 4][i % 4];
+                    weight = fmaxf(weight, at_log2_plus(gv.x, at));
+                    size = fmaxf(size, at_log2_plus(fmaxf(gv.x, fabsf(gv.y) * 0x1p-20f), at));
+                }
+#pragma unroll
+            for (int d = 16; d <= 32; d *= 2) {
+                x = fmaxf(x, kv_xor_f32(x, d));
+                weight = fmaxf(weight, kv_xor_f32(weight, d));
+                size = fmaxf(size, kv_xor_f32(size, d));
+            }
+            const bool first = over[t] < 0.0f, moves = x > over[t] || weight > kAtFull;
+            // (whole numbers: what was summed is scaled by powers of two, without a rounding)
+            const float up = moves ? ceilf(fmaxf(x - kAtFar, size - kAtRoom)) : 0.0f;
+            over[t] = moves ? kAtMost : over[t];
+            m[t] += up;
+            float down = first ? 1.0f : at_power(-up);                // (first: there is nothing to scale)
+#if defined(__AMDGCN__)
+            asm volatile("" : "+v"(down));   // (else lanes that do not move branch past the products, which copies o: 28 registers, a block less a CU)
+#endif
+            l[t] *= down;
+            lv[t] *= down;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) o[t][b] *= down;
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
                 s[u][t][0] -= up;
@@ -616,7 +629,10 @@ template <int D, int NCT, int DT> struct AtWave {
                         if (!there(u) || tok < lo[t] || tok >= hi[t]) x.s[u][t][i / 4][i % 4] = -INFINITY;
                     }
         }
-        bool moves = sv_top > sv_most;
+        // No column moves if its largest score in this lane would not with the largest scale of the lane's tokens, seen or not.  (2^-6 less than what it may
+        // be, for the roundings on both sides: whether a column moves depends on nothing but the column)
+        const float room = kAtFull - 0x1p-6f - at_log2_plus(sv_top, 0.0f);
+        bool moves = false;
 #pragma unroll
         for (int t = 0; t < NCT; ++t) {
             top[t] = x.s[0][t][0][0];
@@ -624,9 +640,9 @@ template <int D, int NCT, int DT> struct AtWave {
             for (int u = 0; u < SUB; ++u)
 #pragma unroll
                 for (int i = u ? 0 : 1; i < 8; ++i) top[t] = fmaxf(top[t], x.s[u][t][i / 4][i % 4]);
-            moves |= top[t] > over[t];
+            moves |= top[t] > fminf(over[t], room);
         }
-        if (__ballot(moves) != 0ull) rescale<SUB>(x.s, top, sv_top);
+        if (__ballot(moves) != 0ull) raise<SUB>(x.s, top, mem);
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
             f16x8 p[NCT][PIECES];
@@ -634,7 +650,7 @@ template <int D, int NCT, int DT> struct AtWave {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float2 gv = mem(u)[32u + 8u * g + i];
-                sv[i] = gv.x * norm;
+                sv[i] = gv.x;
                 bv[i] = gv.y;
             }
 #pragma unroll
@@ -679,21 +695,23 @@ template <int D, int NCT, int DT> struct AtWave {
         __builtin_amdgcn_wave_barrier();
     }
 
-    // The sums of all lanes of a column; o becomes the numerator, m the maximum in log2.
+    // The sums of all lanes of a column; o becomes the numerator.  l is brought to [1/2, 1), so that m of different waves and pieces compare.
     __device__ __forceinline__ void finish()
     {
-        const float back = ldexpf(1.0f, -norm_exp);
 #pragma unroll
         for (int t = 0; t < NCT; ++t) {
             l[t] += kv_xor_f32(l[t], 16);
             l[t] += kv_xor_f32(l[t], 32);
             lv[t] += kv_xor_f32(lv[t], 16);
             lv[t] += kv_xor_f32(lv[t], 32);
-            m[t] = l[t] == 0.0f ? -3.402823466e38f : m[t];   // (a column that saw nothing: below any other)
+            int32_t ex;
+            const bool none = l[t] == 0.0f;
+            l[t] = frexpf(l[t], &ex);
+            m[t] = none ? -3.402823466e38f : m[t] + (float)ex;   // (a column that saw nothing: below any other)
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[t][b][r] = fmaf(o[t][b][r], back, lv[t]);
+                for (int r = 0; r < 4; ++r) o[t][b][r] = ldexpf(o[t][b][r] + lv[t], -ex);
         }
     }
 };
