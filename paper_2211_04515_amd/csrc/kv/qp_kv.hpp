@@ -77,6 +77,21 @@ __device__ __forceinline__ uint32_t kv_wave_scan(uint32_t v)
     return (uint32_t)(x + (row == 0u ? 0 : row == 1u ? a : row == 2u ? b : c));
 }
 
+// A launch has fewer than 2^32 threads; what has more blocks (65536 rows of 1024 heads each) goes in several, and a block's number is blockIdx.x and
+// what its launch is told to add.
+#ifndef QP_KV_GRID
+#define QP_KV_GRID (1u << 23)
+#endif
+template <typename Launch> hipError_t kv_launches(uint64_t blocks, const Launch &launch)
+{
+    hipError_t e = hipSuccess;
+    for (uint64_t b = 0; b < blocks && e == hipSuccess; b += QP_KV_GRID) {
+        launch(dim3((unsigned)(blocks - b < QP_KV_GRID ? blocks - b : QP_KV_GRID)), (uint32_t)b);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
 hipError_t launch_kv_append(const KvLayer &c, uint32_t dim, int dtype, const KvView &k, const KvView &v, hipStream_t s);
 hipError_t launch_kv_read(const KvLayer &c, uint32_t dim, int dtype, const int32_t *first, const KvView &k, const KvView &v,
                           hipStream_t s);

@@ -913,10 +913,10 @@ __device__ __forceinline__ void at_few(const KvLayer &c, const KvView &qv, const
 }
 
 template <int D, int DT>
-__global__ __launch_bounds__(kAtThreads, D <= 128 ? 2 : 1) void k_kv_attention_few(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w)
+__global__ __launch_bounds__(kAtThreads, D <= 128 ? 2 : 1) void k_kv_attention_few(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork w, uint32_t block0)
 {
     __shared__ __align__(16) AtFewLds<D> lds;
-    at_few<D, DT>(c, qv, out, a, w, blockIdx.x, lds);
+    at_few<D, DT>(c, qv, out, a, w, block0 + blockIdx.x, lds);
 }
 
 // Of 32 tokens: the fragments of keys (j, k), then of values, and the grids.
@@ -1034,15 +1034,17 @@ __device__ __forceinline__ void at_many(const KvLayer &c, const KvView &qv, cons
 // Both kinds at once: the rests that are for `few` come behind the others, beside their last work (a launch of their own: 4 rows
 // of 130 new tokens and 1000 in all 58 us, so 47; a prompt of 2048 among 63 single tokens 155, so 148).
 template <int D, int DT>
-__global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? 2 : 1) void k_kv_attention_many(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork few, AtWork many)
+__global__ __launch_bounds__(kAtThreads, D <= 128 && DT == QP_BF16 ? 2 : 1) void k_kv_attention_many(KvLayer c, KvView qv, KvView out, KvAttn a, AtWork few, AtWork many,
+                                                                                                     uint32_t block0)
 {
     union Lds {
         AtFewLds<D> few;
         AtStage<D> many[2][kAtSub<D>];
     };
     __shared__ __align__(16) unsigned char lds[sizeof(Lds)];
-    if (blockIdx.x < many.blocks) at_many<D, DT>(c, qv, out, a, many, blockIdx.x, *reinterpret_cast<AtStage<D>(*)[2][kAtSub<D>]>(lds));
-    else at_few<D, DT>(c, qv, out, a, few, blockIdx.x - many.blocks, *reinterpret_cast<AtFewLds<D> *>(lds));
+    const uint32_t block = block0 + blockIdx.x;
+    if (block < many.blocks) at_many<D, DT>(c, qv, out, a, many, block, *reinterpret_cast<AtStage<D>(*)[2][kAtSub<D>]>(lds));
+    else at_few<D, DT>(c, qv, out, a, few, block - many.blocks, *reinterpret_cast<AtFewLds<D> *>(lds));
 }
 
 // ---- the pieces of a column, joined ----------------------------------------------------------------------------------------
@@ -1172,9 +1174,11 @@ static hipError_t at_launch(const KvLayer &c, const KvView &q, const KvView &out
         hipLaunchKernelGGL(k_kv_plan<D>, dim3(wide ? 2u : 1u), dim3(kAtPlan), 0, s, c, a, few, many);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    if (wide) hipLaunchKernelGGL((k_kv_attention_many<D, DT>), dim3(many.blocks + few.blocks), dim3(kAtThreads), 0, s, c, q, out, a, few, many);
-    else hipLaunchKernelGGL((k_kv_attention_few<D, DT>), dim3(few.blocks), dim3(kAtThreads), 0, s, c, q, out, a, few);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    e = kv_launches((uint64_t)many.blocks + few.blocks, [&](dim3 grid, uint32_t block0) {
+        if (wide) hipLaunchKernelGGL((k_kv_attention_many<D, DT>), grid, dim3(kAtThreads), 0, s, c, q, out, a, few, many, block0);
+        else hipLaunchKernelGGL((k_kv_attention_few<D, DT>), grid, dim3(kAtThreads), 0, s, c, q, out, a, few, block0);
+    });
+    if (e != hipSuccess) return e;
     const uint32_t cols = few.most_cols + many.most_cols;
     if (cols == 0u) return hipSuccess;        // no row is longer than a piece
     hipLaunchKernelGGL((k_kv_join<D, DT>), dim3(cols < kAtJoinBlocks ? cols : kAtJoinBlocks), dim3(kAtThreads), 0, s, out, c.kv_heads * a.group, few, many);

@@ -177,12 +177,12 @@ __device__ __forceinline__ uint32_t kv_codes(const float (&x)[8], const KvGrid &
 
 // `span`: tokens of the call that a wave looks through for octets that begin there
 template <int D, int DT>
-__global__ __launch_bounds__(kKvThreads) void k_kv_append(KvLayer c, KvView k, KvView v, uint32_t span)
+__global__ __launch_bounds__(kKvThreads) void k_kv_append(KvLayer c, KvView k, KvView v, uint32_t span, uint32_t block0)
 {
     constexpr int W = D / kKvCodes;              // words of a token
     constexpr int UNITS = (W + 7) / 8;           // words of a lane
     const uint32_t lane = threadIdx.x % kWave, j = lane / 8u, p = lane % 8u;
-    const uint64_t wave = (uint64_t)blockIdx.x * (kKvThreads / kWave) + threadIdx.x / kWave;
+    const uint64_t wave = ((uint64_t)block0 + blockIdx.x) * (kKvThreads / kWave) + threadIdx.x / kWave;
     const uint32_t head = (uint32_t)(wave % c.kv_heads);
     const uint64_t t0 = wave / c.kv_heads * span;
     if (t0 >= c.tokens) return;
@@ -238,12 +238,12 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvLayer c, KvView k, K
 
 // ---- and back ------------------------------------------------------------------------------------------------------------
 template <int D, int DT>
-__global__ __launch_bounds__(kKvThreads) void k_kv_read(KvLayer c, const int32_t *__restrict__ firsts, KvView k, KvView v, uint32_t span)
+__global__ __launch_bounds__(kKvThreads) void k_kv_read(KvLayer c, const int32_t *__restrict__ firsts, KvView k, KvView v, uint32_t span, uint32_t block0)
 {
     constexpr int W = D / kKvCodes;
     constexpr int UNITS = (W + 7) / 8;
     const uint32_t lane = threadIdx.x % kWave, j = lane / 8u, p = lane % 8u;
-    const uint64_t wave = (uint64_t)blockIdx.x * (kKvThreads / kWave) + threadIdx.x / kWave;
+    const uint64_t wave = ((uint64_t)block0 + blockIdx.x) * (kKvThreads / kWave) + threadIdx.x / kWave;
     const uint32_t head = (uint32_t)(wave % c.kv_heads);
     const uint64_t t0 = wave / c.kv_heads * span;
     if (t0 >= c.tokens) return;
@@ -321,50 +321,58 @@ static uint32_t kv_span(const KvLayer &c)
     if (c.tokens < 8u * (uint64_t)c.rows) return 1u;
     return (uint64_t)c.tokens * c.kv_heads >= 32ull * QP_KV_SPAN_FILL ? 32u : 8u;
 }
-static dim3 kv_rows_grid(const KvLayer &c, uint32_t span)
+static uint64_t kv_rows_blocks(const KvLayer &c, uint32_t span)
 {
     const uint64_t waves = ((uint64_t)c.tokens + span - 1u) / span * c.kv_heads;
-    return dim3((unsigned)((waves + kKvThreads / kWave - 1u) / (kKvThreads / kWave)));
+    return (waves + kKvThreads / kWave - 1u) / (kKvThreads / kWave);
 }
 
-template <int D> static void append_dim(const KvLayer &c, int dtype, const KvView &k, const KvView &v, hipStream_t s)
+template <int D, int DT> static hipError_t append_as(const KvLayer &c, const KvView &k, const KvView &v, hipStream_t s)
 {
     const uint32_t span = kv_span(c);
-    if (dtype == QP_F32) hipLaunchKernelGGL((k_kv_append<D, QP_F32>), kv_rows_grid(c, span), dim3(kKvThreads), 0, s, c, k, v, span);
-    else hipLaunchKernelGGL((k_kv_append<D, QP_BF16>), kv_rows_grid(c, span), dim3(kKvThreads), 0, s, c, k, v, span);
+    return kv_launches(kv_rows_blocks(c, span), [&](dim3 grid, uint32_t block0) {
+        hipLaunchKernelGGL((k_kv_append<D, DT>), grid, dim3(kKvThreads), 0, s, c, k, v, span, block0);
+    });
+}
+template <int D> static hipError_t append_dim(const KvLayer &c, int dtype, const KvView &k, const KvView &v, hipStream_t s)
+{
+    return dtype == QP_F32 ? append_as<D, QP_F32>(c, k, v, s) : append_as<D, QP_BF16>(c, k, v, s);
+}
+template <int D, int DT> static hipError_t read_as(const KvLayer &c, const int32_t *first, const KvView &k, const KvView &v, hipStream_t s)
+{
+    const uint32_t span = kv_span(c);
+    return kv_launches(kv_rows_blocks(c, span), [&](dim3 grid, uint32_t block0) {
+        hipLaunchKernelGGL((k_kv_read<D, DT>), grid, dim3(kKvThreads), 0, s, c, first, k, v, span, block0);
+    });
 }
 template <int D>
-static void read_dim(const KvLayer &c, int dtype, const int32_t *first, const KvView &k, const KvView &v, hipStream_t s)
+static hipError_t read_dim(const KvLayer &c, int dtype, const int32_t *first, const KvView &k, const KvView &v, hipStream_t s)
 {
-    const uint32_t span = kv_span(c);
-    if (dtype == QP_F32) hipLaunchKernelGGL((k_kv_read<D, QP_F32>), kv_rows_grid(c, span), dim3(kKvThreads), 0, s, c, first, k, v, span);
-    else hipLaunchKernelGGL((k_kv_read<D, QP_BF16>), kv_rows_grid(c, span), dim3(kKvThreads), 0, s, c, first, k, v, span);
+    return dtype == QP_F32 ? read_as<D, QP_F32>(c, first, k, v, s) : read_as<D, QP_BF16>(c, first, k, v, s);
 }
 
 hipError_t launch_kv_append(const KvLayer &c, uint32_t dim, int dtype, const KvView &k, const KvView &v, hipStream_t s)
 {
     switch (dim) {
-        case 64: append_dim<64>(c, dtype, k, v, s); break;
-        case 80: append_dim<80>(c, dtype, k, v, s); break;
-        case 96: append_dim<96>(c, dtype, k, v, s); break;
-        case 128: append_dim<128>(c, dtype, k, v, s); break;
-        case 256: append_dim<256>(c, dtype, k, v, s); break;
+        case 64: return append_dim<64>(c, dtype, k, v, s);
+        case 80: return append_dim<80>(c, dtype, k, v, s);
+        case 96: return append_dim<96>(c, dtype, k, v, s);
+        case 128: return append_dim<128>(c, dtype, k, v, s);
+        case 256: return append_dim<256>(c, dtype, k, v, s);
         default: return hipErrorInvalidValue;
     }
-    return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const KvLayer &c, uint32_t dim, int dtype, const int32_t *first, const KvView &k, const KvView &v, hipStream_t s)
 {
     switch (dim) {
-        case 64: read_dim<64>(c, dtype, first, k, v, s); break;
-        case 80: read_dim<80>(c, dtype, first, k, v, s); break;
-        case 96: read_dim<96>(c, dtype, first, k, v, s); break;
-        case 128: read_dim<128>(c, dtype, first, k, v, s); break;
-        case 256: read_dim<256>(c, dtype, first, k, v, s); break;
+        case 64: return read_dim<64>(c, dtype, first, k, v, s);
+        case 80: return read_dim<80>(c, dtype, first, k, v, s);
+        case 96: return read_dim<96>(c, dtype, first, k, v, s);
+        case 128: return read_dim<128>(c, dtype, first, k, v, s);
+        case 256: return read_dim<256>(c, dtype, first, k, v, s);
         default: return hipErrorInvalidValue;
     }
-    return hipGetLastError();
 }
 
 }  // namespace qp

@@ -14,7 +14,7 @@ EMU = os.path.dirname(HERE)
 sys.path.insert(0, EMU)
 import build_emu  # noqa: E402
 
-FLAGS = ["-DQP_KV_FEW=12", "-DQP_KV_MANY=10", "-DQP_KV_LEAST=1", "-DQP_KV_SPAN_FILL=30", "-DQP_KV_COPY_BLOCKS=4"]
+FLAGS = ["-DQP_KV_FEW=12", "-DQP_KV_MANY=10", "-DQP_KV_LEAST=1", "-DQP_KV_SPAN_FILL=30", "-DQP_KV_COPY_BLOCKS=4", "-DQP_KV_GRID=5"]
 
 
 def build():

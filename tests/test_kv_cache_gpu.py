@@ -579,3 +579,42 @@ def test_a_step_replays_from_a_graph(qp):
         for n in ("out", "table", "lengths", "pool", "pages"):
             assert torch.equal(a[n], b[n]), (i, n)
     assert a["lengths"].tolist() == [71, 23, 71, 71]
+
+
+def test_more_blocks_than_a_launch_has(qp):
+    """One token for each of 65536 rows of 1024 heads: 2^24 blocks and more, for append, read and attention.  Three of the rows hold anything;
+    theirs are the answers of calls with these three alone, to the bit, and the others' are 0."""
+    rows, heads, dim, page = 65536, 1024, 64, 32
+    some = torch.tensor([0, 40000, 65535], device="cuda")
+    pages = qp.alloc_kv_pages(3, heads, dim, page)
+    cache = qp.kv_cache(pages, heads, dim, page)
+    table, lengths = torch.full((rows, 1), -1, dtype=torch.int32, device="cuda"), torch.zeros(rows, dtype=torch.int32, device="cuda")
+    table[some, 0], lengths[some] = ints(2, 0, 1), ints(20, 1, 32)
+    r = qp.kv_rows(table, lengths)
+    few = qp.kv_rows(table[some].contiguous(), lengths[some].contiguous())
+    g = torch.Generator("cuda").manual_seed(12)
+    k, v = (torch.randn(53, heads, dim, device="cuda", generator=g).bfloat16() for _ in range(2))
+    qp.qp_kv_append(cache, few, 0, ints(0, 20, 21, 53), k, v)
+    begin = torch.arange(rows + 1, dtype=torch.int32, device="cuda")
+    x = torch.randn(1, heads, dim, device="cuda", generator=g).bfloat16()
+    before = pages.clone()
+    qp.qp_kv_append(cache, few, 0, ints(0, 1, 2, 3), x.expand(3, -1, -1), 2 * x.expand(3, -1, -1))
+    want = pages.clone()
+    pages.copy_(before)
+    qp.qp_kv_append(cache, r, 0, begin, x.expand(rows, -1, -1), (2 * x).expand(rows, -1, -1))
+    assert torch.equal(pages, want)
+
+    def zero(t):
+        t[some] = 0
+        return int(torch.count_nonzero(t.view(torch.int32))) == 0
+
+    q = x.expand(rows, -1, -1)
+    out, same = torch.full((rows, heads, dim), 7, dtype=torch.bfloat16, device="cuda"), torch.empty(3, heads, dim, dtype=torch.bfloat16, device="cuda")
+    qp.qp_kv_attention(cache, r, 0, begin, q, out, qp.alloc_kv_workspace(cache, r, rows, heads))
+    qp.qp_kv_attention(cache, few, 0, ints(0, 1, 2, 3), q[:3], same, qp.alloc_kv_workspace(cache, few, 3, heads))
+    assert torch.equal(out[some], same) and not (same == 0).all(-1).any() and zero(out)
+    vo, first = torch.full_like(out, 7), torch.where(lengths > 0, lengths - 1, 0).int()
+    qp.qp_kv_read(cache, r, 0, begin, out.fill_(7), vo, first=first)
+    k3, v3 = torch.empty_like(same), torch.empty_like(same)
+    qp.qp_kv_read(cache, few, 0, ints(0, 1, 2, 3), k3, v3, first=first[some].contiguous())
+    assert torch.equal(out[some], k3) and torch.equal(vo[some], v3) and zero(out) and zero(vo)
