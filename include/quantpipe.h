@@ -413,7 +413,8 @@ qp_status qp_controller_update(qp_controller_t *c, double payload_bits, double s
  * Tokens of a call.  token_begin_dev[0 .. rows] says which of the `tokens` tokens of the call's tensors belong to which row:
  * row r has tokens token_begin_dev[r] .. token_begin_dev[r + 1] - 1 (ascending; cut off at 0 and `tokens`).  For qp_kv_append and
  * qp_kv_attention they are the row's LAST tokens: lengths_dev counts them already, as qp_kv_reserve leaves it.  (Should a row
- * have more of them than its length, the first ones have no place: they are not stored, and see nothing.)  Tokens that are no row's
+ * have more of them than its length, the first ones have no place: they are not stored, and with causal attention they see nothing; without, they
+ * see the whole row like all others, so that queries need not be the row's own.)  Tokens that are no row's
  * are left alone: not stored, and their place in an output stays as it was.  tokens and tokens * heads are below 2^31.
  *
  * A step of a serving loop is qp_kv_reserve once, then qp_kv_append and qp_kv_attention for each layer.  All calls are

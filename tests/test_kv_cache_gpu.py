@@ -618,3 +618,14 @@ def test_more_blocks_than_a_launch_has(qp):
     k3, v3 = torch.empty_like(same), torch.empty_like(same)
     qp.qp_kv_read(cache, few, 0, ints(0, 1, 2, 3), k3, v3, first=first[some].contiguous())
     assert torch.equal(out[some], k3) and torch.equal(vo[some], v3) and zero(out) and zero(vo)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_without_causality_of_more_tokens_than_the_row_has(qp, dtype):
+    """Queries that are none of the row's tokens: each sees the whole row."""
+    Case(qp, 64, 32, 3, [5, 0, 40, 700]).attend([6, 2, 100, 900], 2, dtype, causal=False)
+    c = Case(qp, 128, 64, 1, [9])
+    q = np.repeat(c.rng.standard_normal((1, 4, 128)).astype(np.float32), 12, 0)
+    out = c.attend([12], 4, dtype, causal=False, q=q)
+    assert torch.equal(out, out[:1].expand(12, 4, 128))
+    assert (c.attend([12], 4, dtype, q=q)[:3] == 0).all()          # causal: three tokens ahead of the row's first

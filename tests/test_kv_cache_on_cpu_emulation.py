@@ -369,3 +369,9 @@ def test_books_that_make_no_sense_stay_inside(driver, tmp_path):
     e.do("free", "keep", "pool")
     e.do("compact", "pool")
     e.run("pool")
+
+
+@pytest.mark.parametrize("lengths,counts,dtype", [([5, 0, 33], [6, 3, 2], 1), ([5, 40], [20, 50], 0)])
+def test_attention_without_causality_of_more_tokens_than_the_row_has(driver, tmp_path, lengths, counts, dtype):
+    """Queries that are none of the row's tokens: each sees the whole row."""
+    attend(driver, tmp_path, 64, 32, 1, 1, lengths, counts, dtype, causal=0)
