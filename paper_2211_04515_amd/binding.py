@@ -403,9 +403,8 @@ def kv_cache(pages, kv_heads: int, head_dim: int, page_tokens: int) -> qp_kv_cac
     """The cache in `pages`: contiguous device bytes of shape [layers, n_pages, ...] (alloc_kv_pages makes them)."""
     if pages.dim() < 2 or pages.dtype != torch.uint8 or not pages.is_contiguous() or not pages.is_cuda:
         raise ValueError("pages: expected a contiguous uint8 device tensor [layers, n_pages, ...]")
-    c = qp_kv_cache_t(pages.data_ptr(), pages.numel(), pages.shape[0], pages.shape[1], kv_heads, head_dim, page_tokens, 0)
-    if qp_kv_page_bytes(c) == 0:
-        raise QuantPipeError(QP_EINVAL, "kv_cache")
+    c = _sizes("kv_cache", pages.shape[0], pages.shape[1], kv_heads, head_dim, page_tokens)
+    c.pages_dev, c.pages_bytes = pages.data_ptr(), pages.numel()
     c.tensors, c.device = (pages,), pages.get_device()
     return c
 
@@ -422,10 +421,10 @@ def kv_rows(table, lengths) -> qp_kv_rows_t:
 
 def alloc_kv_pages(n_pages: int, kv_heads: int, head_dim: int, page_tokens: int, layers: int = 1, device="cuda") -> "torch.Tensor":
     """Room for a cache, not initialised: what was never written is never looked at."""
-    nb = qp_kv_page_bytes(qp_kv_cache_t(None, 0, layers, n_pages, kv_heads, head_dim, page_tokens, 0))
-    if nb == 0:
-        raise QuantPipeError(QP_EINVAL, "qp_kv_page_bytes")
-    return torch.empty((layers, n_pages, kv_heads, nb // kv_heads), dtype=torch.uint8, device=device)
+    c = _sizes("alloc_kv_pages", layers, n_pages, kv_heads, head_dim, page_tokens)
+    if not (1 <= layers <= 65536 and 1 <= n_pages <= 1 << 24):
+        raise QuantPipeError(QP_EINVAL, "alloc_kv_pages")
+    return torch.empty((layers, n_pages, kv_heads, qp_kv_page_bytes(c) // kv_heads), dtype=torch.uint8, device=device)
 
 
 def alloc_kv_pool(n_pages: int, device="cuda") -> "torch.Tensor":
@@ -482,6 +481,14 @@ def _uint(v: int, what: str) -> int:
     return int(v)
 
 
+def _sizes(what: str, *sizes) -> qp_kv_cache_t:
+    """A cache of these sizes (layers, n_pages, kv_heads, head_dim, page_tokens), without its pages."""
+    c = qp_kv_cache_t(None, 0, *(_uint(v, what) for v in sizes), 0)
+    if qp_kv_page_bytes(c) == 0:
+        raise QuantPipeError(QP_EINVAL, what)
+    return c
+
+
 def qp_kv_page_bytes(cache: qp_kv_cache_t) -> int:
     return int(lib().qp_kv_page_bytes(C.byref(cache)))
 
@@ -491,10 +498,14 @@ def qp_kv_pool_bytes(n_pages: int) -> int:
 
 
 def qp_kv_attention_workspace_bytes(cache: qp_kv_cache_t, rows: qp_kv_rows_t, tokens: int, q_heads: int) -> int:
+    if not (0 <= tokens < 1 << 32 and 0 <= q_heads < 1 << 32):
+        return 0
     return int(lib().qp_kv_attention_workspace_bytes(C.byref(cache), C.byref(rows), int(tokens), int(q_heads)))
 
 
 def qp_kv_pool_init(n_pages: int, pool, stream=None) -> None:
+    if qp_kv_pool_bytes(n_pages) == 0:
+        raise QuantPipeError(QP_EINVAL, "qp_kv_pool_init")
     d = pool.get_device()
     _kv_call(d, stream, "qp_kv_pool_init", int(n_pages), _ints(pool, 1, d), pool.numel() * 4)
 

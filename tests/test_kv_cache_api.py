@@ -182,3 +182,19 @@ def test_the_binding_refuses_tensors_of_other_kinds(qp):
         qp.alloc_kv_pool(0, device="cpu")
     with pytest.raises(qp.QuantPipeError):
         qp.alloc_kv_pool(2 ** 32 + 5, device="cpu")
+
+
+def test_the_binding_refuses_numbers_past_32_bits(qp):
+    """ctypes would cut them down to their low 32 bits: 2^32 + 4 pages to 4, 2^32 + 8 heads to 8."""
+    for n in (2 ** 32 + 4, -4, 0):
+        with pytest.raises(qp.QuantPipeError):
+            qp.qp_kv_pool_init(n, torch.zeros(1000, dtype=torch.int32))
+    for kind in ((2 ** 32 + 1, 64, 32), (1, 2 ** 32 + 64, 32), (1, 64, 2 ** 32 + 32), (-1, 64, 32)):
+        with pytest.raises(qp.QuantPipeError):
+            qp.alloc_kv_pages(4, *kind, device="cpu")
+    for n, layers in ((2 ** 32 + 4, 1), (4, 2 ** 32 + 1), (0, 1), (4, 0), (-1, 1), (4, -1), (2 ** 24 + 1, 1), (4, 65537)):
+        with pytest.raises(qp.QuantPipeError):
+            qp.alloc_kv_pages(n, 1, 64, 32, layers=layers, device="meta")
+    a = make(qp)
+    for tokens, heads in ((7, 2 ** 32 + 8), (2 ** 64 + 7, 8), (-1, 8), (7, -8)):
+        assert qp.qp_kv_attention_workspace_bytes(a["cache"], a["row"], tokens, heads) == 0

@@ -629,3 +629,14 @@ def test_without_causality_of_more_tokens_than_the_row_has(qp, dtype):
     out = c.attend([12], 4, dtype, causal=False, q=q)
     assert torch.equal(out, out[:1].expand(12, 4, 128))
     assert (c.attend([12], 4, dtype, q=q)[:3] == 0).all()          # causal: three tokens ahead of the row's first
+
+
+def test_sizes_past_32_bits_are_refused(qp):
+    pages = qp.alloc_kv_pages(4, 1, 64, 32)
+    for kind in ((2 ** 32 + 1, 64, 32), (1, 2 ** 32 + 64, 32), (1, 64, 2 ** 32 + 32)):
+        with pytest.raises(qp.QuantPipeError):
+            qp.kv_cache(pages, *kind)
+    pool = torch.full((100,), 7, dtype=torch.int32, device="cuda")
+    with pytest.raises(qp.QuantPipeError):
+        qp.qp_kv_pool_init(2 ** 32 + 4, pool)
+    assert (pool == 7).all()
