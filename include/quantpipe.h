@@ -490,16 +490,16 @@ qp_status qp_kv_read(const qp_kv_cache_t *cache, const qp_kv_rows_t *rows, uint3
                      const int32_t *first_dev, uint64_t tokens, const qp_kv_view_t *k, const qp_kv_view_t *v, void *stream);
 
 /* ---- attention over the cache ----------------------------------------------------------
- * out = softmax(scale * q K^T) V for each of the call's tokens and each of q_heads query heads; query head h goes with key head
- * h div (q_heads / kv_heads).  causal: token i of a row's m, at position p = length - m + i, sees tokens t <= p, and with window > 0
- * only t > p - window; without causal it sees the whole row (window must be 0).  A query that sees nothing gives 0; one
- * that holds NaN or Inf gives NaN, and no other query does.  Products take the codes as they are (no value is rounded), bf16
- * queries too (elements below 2^-14 to 2^-29), fp32 queries to 22 bits; a weight times its token's value scale to 11 bits
- * (bf16) or 22 (fp32), and to 2^-31 of the largest such product among the tokens that the query sees (of value scales below 2^-82 or above 2^100
- * to fewer); scores, sums and numerators are fp32; out has q's type.  Where lengths and ranges are the same, an answer is the same to the bit
- * whatever the tokens that its query does not see, other heads and other queries hold.  Long rows are split among blocks and joined in a fixed order: results are the same on
- * every run.  out may be q itself (the same strides); otherwise it overlaps neither q nor the cache.  The workspace needs no
- * initialisation; calls that may run at the same time (two streams, two graphs) need one each. */
+ * out = softmax(scale * q K^T) V for each of the call's tokens and each of q_heads query heads; query head h goes with key head h div (q_heads
+ * / kv_heads).  causal: token i of a row's m, at position p = length - m + i, sees tokens t <= p, and with window > 0 only t > p - window;
+ * without causal it sees the whole row (window must be 0).  A query that sees nothing gives 0; one that holds NaN or Inf gives NaN, and no
+ * other query does.  Products take the codes as they are (no value is rounded), bf16 queries too (elements below 2^-14 to 2^-29), fp32 queries
+ * to 22 bits; a weight times its token's value scale to 11 bits (bf16) or 22 (fp32), and to 2^-31 of the largest such product among the tokens
+ * that the query sees or 2^-114 of the largest weight, whichever is more (value scales up to 2^100); scores, sums and numerators are fp32; out
+ * has q's type.  Where lengths and ranges are the same, an answer is the same to the bit whatever the tokens that its query does not see,
+ * other heads and other queries hold.  Long rows are split among blocks and joined in a fixed order: results are the same on every run.  out
+ * may be q itself (the same strides); otherwise it overlaps neither q nor the cache.  The workspace needs no initialisation; calls that may
+ * run at the same time (two streams, two graphs) need one each. */
 typedef struct {
     float    scale;            /* > 0, finite */
     uint32_t q_heads;          /* a multiple of kv_heads, at most 1024 times it */

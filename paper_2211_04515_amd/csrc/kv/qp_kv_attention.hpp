@@ -13,7 +13,7 @@
 //              that it has seen lies between 2^6, when m was last moved, and 2^15.6: nothing overflows, and what is lost at the lower end is 2^-31 of
 //              the largest.  Of the tokens that the column sees, with the weight that it gives them: one reference for all columns of a wave, or one
 //              from the scales alone, lets a token with a vast value take the bits of columns that do not see or weigh it.  p_t itself stays
-//              below 2^96, which sums in fp32 hold; value scales below 2^-82 have fewer bits for it.
+//              below 2^96, which sums in fp32 hold, so where the largest p_t s_t is less than 2^-83 of the largest p_t, what is lost is 2^-114 of that.
 //   Scores, sum p_t, sum p_t (lo_t + 8 s_t) and the accumulators are fp32.  m is a whole number, so that moving it rounds nothing.
 //
 // Matrix shape.  v_mfma_f32_16x16x32_f16 with S^T = K q^T (16 tokens x 16 columns; a column is one token of the call and one of the

@@ -64,7 +64,9 @@ class World:
                       the reference, which is that less log2 of the largest p s); an answer moves by p_t r_t (|v_t| + W) at most, 1.1 for what
                       is of second order
           sums        n + 64 additions: 2 (n + 64) u W for numerator and denominator
-          p s         to fp16, 2^-11 of it, or in two halves, 2^-22; at least 2^-25 where the largest p max(s, 2^-20 |b|) is 2^6 or more
+          p s         to fp16, 2^-11 of it, or in two halves, 2^-22; at least 2^-25 where the largest p max(s, 2^-20 |b|) is 2^6 or more,
+                      or the largest p 2^89
+          range       weights below 2^-126, which are 0, are less than 2^-132 of the answer's largest p s and more, in its units; fp32's smallest step
           out         half a step of its type
         """
         dim, heads = self.dim, self.heads
@@ -91,10 +93,11 @@ class World:
                     B = scale * (np.abs(x) @ kb[see].T)
                     W = p @ (s8 + b)[see]
                     most = (p * np.maximum(s8 / 8, 2.0 ** -20 * b)[see]).max(1)
-                    L = np.abs(np.log2(most)) + 8
+                    L = np.abs(np.log2(np.maximum(most, 2.0 ** -104))) + 8     # (never further, whatever the sizes: p stays below 2^96)
                     rt = (dim + 16) * U * B + (2.0 ** -22 if dtype == F32 else 2.0 ** -24) * B + 4 * U * (1 + np.abs(z) + np.abs(z).max(1, keepdims=True) + L[:, None])
                     off = 1.1 * (p * rt * ((s8 + b)[see][None] + W[:, None])).sum(1) + 2 * (see.sum() + 64) * U * W
-                    off += split * (p @ s8[see]) + see.sum() * 8 * 2.0 ** -31 * most
+                    off += split * (p @ s8[see]) + see.sum() * 8 * np.maximum(2.0 ** -31 * most, 2.0 ** -114)
+                    off += see.sum() * 2.0 ** -132 * most * ((s8 + b)[see].max() + W) + 2.0 ** -148
                     out[at + i, h * group:(h + 1) * group] = o
                     tol[at + i, h * group:(h + 1) * group] = off[:, None] + u_out * np.abs(o)
             at += m
