@@ -513,11 +513,16 @@ template <int D, int NCT, int DT> struct AtWave {
     // `s`: scores relative to m, which follow; `top`: this lane's largest ones; `mem`: as in weigh
     template <int SUB, typename Mem> __device__ __forceinline__ void raise(f32x4 (&s)[SUB][NCT][2], const float (&top)[NCT], const Mem &mem)
     {
-        const uint32_t g = threadIdx.x % kWave / 16u;
+        uint32_t lane = threadIdx.x % kWave;
+#if defined(__AMDGCN__)
+        asm volatile("" : "+v"(lane));       // (else what follows from it is kept in registers for this branch)
+#endif
+        const uint32_t g = lane / 16u, n = lane % 16u;
 #pragma unroll
         for (int t = 0; t < NCT; ++t) {
             // log2 of the largest p s, and of the largest p times what counts as a token's size: |lo + 8 s| too, far down, for lv's sake
-            float x = top[t], weight = -INFINITY, size = -INFINITY;
+            const float x = top[t];
+            float weight = -INFINITY, size = -INFINITY;
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -527,15 +532,13 @@ template <int D, int NCT, int DT> struct AtWave {
                     weight = fmaxf(weight, at_log2_plus(gv.x, at));
                     size = fmaxf(size, at_log2_plus(fmaxf(gv.x, fabsf(gv.y) * 0x1p-20f), at));
                 }
-#pragma unroll
-            for (int d = 16; d <= 32; d *= 2) {
-                x = fmaxf(x, kv_xor_f32(x, d));
-                weight = fmaxf(weight, kv_xor_f32(weight, d));
-                size = fmaxf(size, kv_xor_f32(size, d));
-            }
-            const bool first = over[t] < 0.0f, moves = x > over[t] || weight > kAtFull;
+            // a column's lanes are n, n + 16, n + 32, n + 48
+            const bool first = over[t] < 0.0f, moves = (__ballot(x > over[t] || weight > kAtFull) >> n & 0x0001000100010001ull) != 0ull;
+            float by = fmaxf(x - kAtFar, size - kAtRoom);
+            by = fmaxf(by, kv_xor_f32(by, 16));
+            by = fmaxf(by, kv_xor_f32(by, 32));
             // (whole numbers: what was summed is scaled by powers of two, without a rounding)
-            const float up = moves ? ceilf(fmaxf(x - kAtFar, size - kAtRoom)) : 0.0f;
+            const float up = moves ? ceilf(by) : 0.0f;
             over[t] = moves ? kAtMost : over[t];
             m[t] += up;
             float down = first ? 1.0f : at_power(-up);                // (first: there is nothing to scale)
