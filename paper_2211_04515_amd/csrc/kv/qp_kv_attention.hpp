@@ -32,17 +32,18 @@
 //   few    16 columns; every wave all of them and every fourth 32 tokens, joined through LDS at the end.  What a single token of a
 //          row, or a few of them, need: bound by HBM, (head_dim + 16) bytes for each token and key head.
 //   many   128 columns, 32 a wave; all waves the same tokens, whose words each wave takes apart a quarter of and shares through
-//          LDS.  Prompts: bound by issue: 12 vector instructions for each score (3 for taking codes apart) beside two matrix ones for 16.
+//          LDS.  Prompts: 12 vector instructions for each score (3 for taking codes apart) beside two matrix ones for 16.
 // A call whose rows bring 16 columns or fewer on average goes to `few` alone; else rows are cut into 128 columns for `many`, and
 // a rest of 16 or fewer goes to `few`, in the same launch (single tokens in a batch with prompts).  Rows' lengths are known to the device only: every
 // wave adds up the whole call's work from them (a row a lane; of more than 64 rows a small kernel ahead does it once) and finds which
 // item, and which of S equal pieces of its tokens, is its block's, so that about as many pieces come out as the chip runs at a time,
 // whatever the lengths.  Pieces leave (m, sum p, numerators) in the workspace, sum p brought to [1/2, 1), and a last kernel joins them in order.
 //
-// Measured (bf16, heads of 128): one token each for 4 rows of up to 131072 (8 key heads, 64 of queries) 113 us, 4.9 TB/s, which is a large
-// copy's rate (4.7); for 32 rows of up to 4096 34 us, 3.0 TB/s, of which joining and finding work are 6; a prompt of 8192 tokens (4 key heads,
-// 16 of queries) 362 us, 760 TFLOP/s, where a large library product in fp16 runs at 1220: vector instructions take 61 % of the SIMDs'
-// cycles and matrix ones 36 %.
+// Measured (bf16, heads of 128): one token each for 4 rows of up to 131072 (8 key heads, 64 of queries) 114 us, 4.9 TB/s, where a loop that only
+// reads reaches 5.9 to 6.7; for 32 rows of up to 4096 33 us, 3.1 TB/s, of which joining and finding work are 6; a prompt of 8192 tokens (4 key
+// heads, 16 of queries) 358 us, 768 TFLOP/s, where a large library product in fp16 runs at 1220.  Of the SIMDs' clocks there 59 % are vector
+// instructions' and 30 % the matrix unit's: neither is full.  A wave spends half of its time in instructions, 27 % waiting for its turn to issue one
+// and 23 % for data and barriers, which two waves a SIMD do not cover for each other.
 #pragma once
 
 #include "qp_kv.hpp"
@@ -54,14 +55,18 @@ constexpr uint32_t kAtStep = 32;                 // tokens of a wave's step
 constexpr uint32_t kAtTile = kAtStep * kAtWaves; // tokens that work is counted in
 constexpr uint32_t kAtUnit = 16;                 // columns that partial results are counted in
 template <bool MANY> constexpr uint32_t kAtCols = MANY ? 128u : kAtUnit;     // columns of an item
-// Blocks that run at the same time: a call is cut into no more pieces than that, if it can be.
+// The pieces that a call is cut into, no more if it can be.  Set for the blocks that run at the same time with bf16 heads of 128 (two waves a SIMD for
+// many columns, three for few); at_launch takes fewer where it says so.  What registers and LDS leave room for at other sizes, waves a SIMD, which is
+// blocks a CU: few columns 4 (64, and 80 in bf16), 3 (80 in fp32, 96, 128 in bf16), 2 (128 in fp32), 1 (256); many columns 2 in bf16 up to 128, else 1,
+// and the few columns' items in the same launch run at that too.  So fp32 prompts of heads up to 96 are cut for twice the blocks that run, and few
+// columns of 256 for 512, of heads of 64 for 768 of 1024.
 #ifndef QP_KV_FEW
 #define QP_KV_FEW 768
 #endif
 #ifndef QP_KV_MANY
 #define QP_KV_MANY 512
 #endif
-template <bool MANY> constexpr uint32_t kAtSlots = MANY ? QP_KV_MANY : QP_KV_FEW;     // at most: three, two blocks a CU
+template <bool MANY> constexpr uint32_t kAtSlots = MANY ? QP_KV_MANY : QP_KV_FEW;
 // Tiles that a piece has at least: joining costs a kernel and a pass over the pieces, more than it takes to go through these.
 #ifndef QP_KV_LEAST
 #define QP_KV_LEAST 4
@@ -85,7 +90,7 @@ struct AtWork {
     float *nums;
     uint32_t most_cols, most_units;
     uint32_t wide;                               // rows are cut into 128 columns first
-    uint32_t slots;                              // blocks that run at the same time
+    uint32_t slots;                              // pieces that the call is to be cut into
     uint32_t blocks;                             // of the launch
 };
 constexpr size_t kAtHeader = 256;
@@ -278,7 +283,8 @@ __device__ __forceinline__ uint64_t at_wave_sum(uint64_t v)
 }
 
 // With more rows than a wave has lanes, one block for each kind of items adds the rows up ahead of them: else every block would, and 4096 rows
-// of up to 500 tokens took 1356 us, so 580; 20000 of 200 17.6 ms, so 2.0; 1024 of 1000 302, so 251; 96 of 1000 30, so 34, which is the launch.
+// of up to 500 tokens took 1356 us, so 580; 20000 of 200 17.6 ms, so 2.0; 1024 of 1000 302, so 251.  (Where it begins is the wave's size, no
+// measured crossing: 96 rows of 1000 took 30 us, so 34, which is the launch.)
 constexpr uint32_t kAtPlan = 1024;
 template <bool MANY> __device__ __forceinline__ void at_plan(const KvLayer &c, const KvAttn &a, const AtWork &w)
 {
@@ -1168,7 +1174,7 @@ static hipError_t at_launch(const KvLayer &c, const KvView &q, const KvView &out
     (void)at_bytes(c, D, a.group, few_bytes);
     AtWork few = at_work<false>(ws, c, D, a.group, bytes);
     AtWork many = wide ? at_work<true>(ws + few_bytes, c, D, a.group, bytes) : AtWork{};
-    if (D == 256 || (D == 128 && DT == QP_F32)) {      // their registers leave room for a block less a CU
+    if (D == 256 || (D == 128 && DT == QP_F32)) {      // (one block a CU with many columns; with few two of 128 in fp32, one of 256)
         few.slots = kAtSlots<false> * 2u / 3u;
         many.slots = kAtSlots<true> / 2u;
     }

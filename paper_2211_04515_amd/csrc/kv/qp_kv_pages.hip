@@ -6,7 +6,8 @@
 // pool (the lowest free page first), which one block of 1024 lanes keeps with prefix sums: it reads 32 KB of reference counts at a
 // time.  Sharing and giving up only add to counts, whose order does not matter.
 // The copy kernel is bound by HBM: 16-byte loads and stores, all layers' pages of a list spread over the whole chip.  Measured: 117 us where
-// 16 layers' pages of 48 requests move together (232 of 1.2 MB), 126 with the books before it, 4.7 TB/s read and written, a large plain copy's rate.
+// 16 layers' pages of 48 requests move together (266 of 1.2 MB on average), 126 with the books before it, 5.4 TB/s read and written (a plain copy of
+// 4 GiB: 4.7).
 // A beam step (8 requests of 5 beams: free, fork, reserve, 32 pages of 16 layers copied) is 29 us: 16.4 of copying (4.6 TB/s), 7.8 to reserve,
 // 3.5 to fork, 2.8 to free.
 #include "qp_kv.hpp"

@@ -8,7 +8,9 @@
 // wave of the call writes them, because all of the call's tokens of a word are this wave's.
 // Bound by HBM: (2 or 4) bytes in and 1/2 + 8/head_dim out for each element, or the reverse.  Measured: 4 rows of up to 32768 tokens read
 // back to bf16 (8 heads of 128) in 111 us, 4.6 TB/s, a large copy's rate; 5 prompts of 1777 tokens in fp32 (12 heads of 64) written in
-// 17.2 us and read in 13.7; one token for each of 64 rows 5.9 us either way, which is the launch and a chain of three loads.
+// 17.2 us and read in 13.7; one token for each of 64 rows 5.9 us either way, which is the launch and a chain of dependent
+// loads: two rounds of the search for the row (of 65 entries), its range and length, its page, then the token's elements and the word that
+// they are merged into; reading back, the grid and codes.
 #include "qp_kv.hpp"
 
 namespace qp {
