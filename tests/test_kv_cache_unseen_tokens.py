@@ -257,7 +257,7 @@ def test_values_of_every_size_emulated(driver, tmp_path, lengths, counts, dtype)
 @pytest.mark.gpu
 @TYPES
 @pytest.mark.parametrize("factor", [1e6, 1e9, 1e30])
-@pytest.mark.parametrize("lengths,counts,group", [([40], [2], 1), ([700, 1, 97], [3, 1, 5], 1), ([150], [140], 1), ([900, 130], [150, 33], 4)])
+@pytest.mark.parametrize("lengths,counts,group", [([40], [2], 1), ([700, 1, 97], [3, 1, 5], 1), ([150], [140], 1), ([900, 130], [150, 33], 4), ([3000], [4], 2)])
 def test_vast_last_token(lengths, counts, group, factor, dtype):
     vast_last_token(on_gpu(), lengths, counts, group, factor, dtype)
 
@@ -286,6 +286,6 @@ def test_vast_token_without_weight(lengths, counts, group, dtype):
 
 @pytest.mark.gpu
 @TYPES
-@pytest.mark.parametrize("lengths,counts", [([70, 1000], [2, 1]), ([500], [100])])
+@pytest.mark.parametrize("lengths,counts", [([70, 1000], [2, 1]), ([500], [100]), ([4000], [3])])
 def test_values_of_every_size(lengths, counts, dtype):
     values_of_every_size(on_gpu(), lengths, counts, dtype)
