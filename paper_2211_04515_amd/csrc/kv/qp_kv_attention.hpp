@@ -9,9 +9,10 @@
 // them: -8..7 costs about as much as the values' own spread would.)
 //   q          is taken as 16 q in fp16: exact for bf16 (what is below 2^-14 rounds at 2^-29); fp32 is split in two halves, 22 bits
 //              of each element.  A column whose largest element lies outside [2^-4, 2^11) gets a power of two of its own.
-//   p_t s_t    is rounded to fp16 (fp32: split in two).  m is no maximum of the scores but the column's own reference, such that the largest p_t s_t
-//              that it has seen lies between 2^6, when m was last moved, and 2^15.6: nothing overflows, and what is lost at the lower end is 2^-31 of
-//              the largest.  Of the tokens that the column sees, with the weight that it gives them: one reference for all columns of a wave, or one
+//   p_t s_t    is rounded to fp16 (fp32: split in two).  One half does for bf16 answers, whose own rounding is 1.66e-3 of them in the 2-norm: with
+//              the weights' it is 1.68e-3, and one answer in ten rounds to the other neighbour.  Two would double the second product.
+//              m is no maximum of the scores but the column's own reference, such that the largest p_t s_t that it has seen lies between 2^6, when m
+//              was last moved, and 2^15.6: nothing overflows, and what is lost at the lower end is 2^-31 of the largest.  Of the tokens that the column sees, with the weight that it gives them: one reference for all columns of a wave, or one
 //              from the scales alone, lets a token with a vast value take the bits of columns that do not see or weigh it.  p_t itself stays
 //              below 2^96, which sums in fp32 hold, so where the largest p_t s_t is less than 2^-83 of the largest p_t, what is lost is 2^-114 of that.
 //   Scores, sum p_t, sum p_t (lo_t + 8 s_t) and the accumulators are fp32.  m is a whole number, so that moving it rounds nothing.
